@@ -164,8 +164,7 @@ def _own_logp(s, case):
     out = pol.log_probs(s["logits"], s["tokens"], mask=s["mask"], top=case["top"])
     if not case["train"]:
         return out
-    return out, pol.log_probs_grad(s["dlogp"], s["dentropy"], s["logits"], s["tokens"], out["lse"], out["entropy"],
-                                   mask=s["mask"])
+    return out, pol.log_probs_grad(s["dlogp"], s["dentropy"], s["logits"], s["tokens"], out, mask=s["mask"])
 
 
 def _own_ffn(s, case):
@@ -229,19 +228,19 @@ def _plain_logp(s, case):
     some = top > -math.inf  # rows with an entry left
     e = torch.exp(x - torch.where(some, top, torch.zeros_like(top)))
     total = e.sum(1, keepdim=True)
-    lse = torch.where(some, top + torch.log(total), top)
-    logs = torch.where(some & (x > -math.inf), x - lse, torch.full_like(x, -math.inf))
+    logz = torch.where(some, torch.log(total), top)
+    logs = torch.where(some & (x > -math.inf), (x - top) - logz, torch.full_like(x, -math.inf))
     p = e / torch.where(some, total, torch.ones_like(total))
     entropy = -(p * torch.where(p > 0, logs, torch.zeros_like(p))).sum(1)
     given = (tok >= 0) & (tok < case["V"])
     at = torch.where(given, tok, torch.zeros_like(tok))[:, None]
     out = dict(logp=torch.where(given, logs.gather(1, at)[:, 0], torch.zeros_like(entropy)), entropy=entropy,
-               lse=lse[:, 0])
+               peak=top[:, 0], logz=logz[:, 0])
     if case["top"]:
         best, index = torch.sort(x, dim=1, descending=True, stable=True)
         best, index = best[:, :case["top"]], index[:, :case["top"]]
         there = best > -math.inf
-        out["top_logp"] = torch.where(there, best - lse, best)
+        out["top_logp"] = torch.where(there, (best - top) - logz, best)
         out["top_index"] = torch.where(there, index, torch.full_like(index, -1)).to(torch.int32)
     if not case["train"]:
         return out
@@ -327,7 +326,8 @@ def _exact_logp(s, case):
     entropy = torch.special.entr(p).sum(1)
     absent = (tok < 0) | (tok >= case["V"])
     logp = logs.gather(1, tok.masked_fill(absent, 0)[:, None])[:, 0].masked_fill(absent, 0.0)
-    out = dict(logp=logp, entropy=entropy, lse=lse)
+    peak = x.amax(1)
+    out = dict(logp=logp, entropy=entropy, peak=peak, logz=(lse - peak).masked_fill(dead, -math.inf))
     if case["top"]:
         out["top_logp"], out["top_index"] = logs.topk(case["top"], dim=1).values, None
     if not case["train"]:
