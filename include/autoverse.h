@@ -371,6 +371,122 @@ int av_rollout_path(av_handle *h, int32_t *path);
  * Writes the path to *path; AV_EINVAL for a null argument.  No GPU work. */
 int av_step_path(av_handle *h, int32_t *path);
 
+/* ------------------------------------------------------------------ policy
+ * The pieces of a recurrent policy that acts in the environments and learns
+ * from their trajectories (Sec. 3.2 behaviour cloning, Sec. 3.3 reinforcement
+ * learning).  No handle: arrays and workspaces are caller-owned device memory,
+ * work is enqueued on `stream` without synchronising, argument errors give
+ * AV_EINVAL before any launch and a failed launch AV_ECUDA.  Calls allocate
+ * nothing and can be captured in a graph; calls on other streams may overlap
+ * as long as their outputs and workspaces are their own.  Outputs overlap no
+ * input and no other output unless said otherwise.  Strides are in elements;
+ * innermost axes are contiguous.  Every sum, softmax statistic and recurrent
+ * state is held in 32 bits whatever the arrays' type, and no result depends on
+ * the order in which blocks run: equal inputs give equal bits. */
+enum { AV_F32 = 0, AV_BF16 = 1, AV_F16 = 2 }; /* value types, `dtype` below */
+
+/* Layer norm of rows x [rows][n] (row stride x_stride): mean and variance of
+ * each row, rstd = 1 / sqrt(var + eps), y = (x - mean) rstd weight + bias.
+ * weight, bias: [n] of type param_dtype, each may be NULL (1, 0).  mean, rstd:
+ * float [rows] for av_layer_norm_grad, or both NULL.  y has x's type. */
+int av_layer_norm(int64_t rows, int32_t n, int32_t dtype, int32_t param_dtype, float eps,
+                  const void *x, int64_t x_stride, const void *weight, const void *bias, void *y,
+                  int64_t y_stride, float *mean, float *rstd, uintptr_t stream);
+
+/* Its gradient: with xh = (x - mean) rstd and d = dy weight,
+ *   dx = rstd (d - mean(d) - xh mean(d xh)),  dweight = sum dy xh,  dbias = sum dy
+ * (sums over the rows; dweight and dbias, [n] of param_dtype, may be NULL).
+ * work: av_layer_norm_work bytes, 16-byte aligned. */
+int av_layer_norm_grad(int64_t rows, int32_t n, int32_t dtype, int32_t param_dtype, const void *dy,
+                       int64_t dy_stride, const void *x, int64_t x_stride, const void *weight,
+                       const float *mean, const float *rstd, void *dx, int64_t dx_stride,
+                       void *dweight, void *dbias, void *work, int64_t work_bytes,
+                       uintptr_t stream);
+int av_layer_norm_work(int64_t rows, int32_t n, int64_t *bytes);
+
+/* Gated linear recurrence over T steps of B sequences with D channels:
+ *   a = sigmoid(gate_t),  h_t = a k_t h_{t-1} + (1 - a) value_t,
+ * k_t = 0 where reset_t is not 0 (an episode begins at t: what came before is
+ * forgotten), else 1.  gate, value, h: [T][B][D] with strides of their own for
+ * steps and sequences; reset: uint8 [T][B] with strides, or NULL; h0: float
+ * [B][D], the state before step 0, or NULL (zeros); h_last: float [B][D], the
+ * state after step T - 1 (unrounded), or NULL; it may be h0 itself.
+ * states: float [av_scan_sizes' states], kept for av_scan_grad, or NULL.
+ * work: av_scan_sizes' work bytes, 16-byte aligned (may be NULL when 0).
+ * Long sequences are split over blocks that wait for their predecessors'
+ * states.  Each wait has a limit of some seconds; past it the block writes
+ * NaN in place of its outputs, so that no wrong state passes for a right one. */
+int av_scan(int64_t T, int64_t B, int64_t D, int32_t dtype, const void *gate, int64_t gate_t,
+            int64_t gate_b, const void *value, int64_t value_t, int64_t value_b,
+            const uint8_t *reset, int64_t reset_t, int64_t reset_b, const float *h0, void *h,
+            int64_t h_t, int64_t h_b, float *h_last, float *states, void *work, int64_t work_bytes,
+            uintptr_t stream);
+
+/* Its gradient, from dh (of h) and dlast (float [B][D], of h_last, or NULL):
+ *   l_t = dh_t + a_{t+1} k_{t+1} l_{t+1}, dlast added to l_{T-1},
+ *   dvalue_t = (1 - a_t) l_t,  dgate_t = l_t (k_t h_{t-1} - value_t) a_t (1 - a_t),
+ *   dh0 = a_0 k_0 l_0  (float [B][D], or NULL).
+ * gate, value, reset are av_scan's and states what it kept. */
+int av_scan_grad(int64_t T, int64_t B, int64_t D, int32_t dtype, const void *dh, int64_t dh_t,
+                 int64_t dh_b, const void *gate, int64_t gate_t, int64_t gate_b, const void *value,
+                 int64_t value_t, int64_t value_b, const uint8_t *reset, int64_t reset_t,
+                 int64_t reset_b, const float *states, const float *dlast, void *dgate,
+                 int64_t dgate_t, int64_t dgate_b, void *dvalue, int64_t dvalue_t, int64_t dvalue_b,
+                 float *dh0, void *work, int64_t work_bytes, uintptr_t stream);
+/* states: floats that av_scan keeps; work: bytes that either call works in. */
+int av_scan_sizes(int64_t T, int64_t B, int64_t D, int32_t dtype, int64_t *states, int64_t *work);
+
+#define AV_MAX_TOP 32 /* alternatives returned by av_log_probs */
+
+/* Log probabilities under the softmax of logits [rows][V] (row stride
+ * logit_stride).  With peak the row's largest logit, logz = log sum exp(x - peak)
+ * and log p_j = (x_j - peak) - logz: logp of the row's token, entropy =
+ * - sum p log p, peak and logz (float [rows] each; all but logp may be NULL;
+ * kept apart, peak and logz give log p its full precision however large the
+ * logits are; their sum is the row's log sum exp), and
+ * the `top` (0..min(V, AV_MAX_TOP)) largest, in order, the lowest index first
+ * among equals, NaN before all: top_logp float [rows][top], top_index int32
+ * [rows][top].  tokens: [rows] of token_bytes 1 (uint8), 4 (int32) or 8
+ * (int64); a token outside 0..V-1 gives logp 0 and no gradient.  mask: uint8
+ * [rows][V] (row stride mask_stride, 0 = one for all) or NULL: entries with 0
+ * are not there, whatever their logit (NaN among them).  Entries of logit -inf
+ * have probability 0.  A row with nothing left has peak = logz = logp = -inf
+ * and entropy 0; alternatives that are not there have index -1 and -inf.  NaN
+ * or +inf among a row's entries makes its logz, logp and entropy NaN. */
+int av_log_probs(int64_t rows, int32_t V, int32_t dtype, const void *logits, int64_t logit_stride,
+                 const void *tokens, int32_t token_bytes, const uint8_t *mask, int64_t mask_stride,
+                 int32_t top, float *logp, float *entropy, float *peak, float *logz,
+                 float *top_logp, int32_t *top_index, uintptr_t stream);
+
+/* Its gradient, from that of logp and of entropy (float [rows], each may be
+ * NULL = 0) and what av_log_probs gave (entropy may be NULL with dentropy):
+ *   dx_j = dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy),
+ * 0 for entries masked and rows with nothing left.  dlogits has logits' type. */
+int av_log_probs_grad(int64_t rows, int32_t V, int32_t dtype, const void *logits,
+                      int64_t logit_stride, const void *tokens, int32_t token_bytes,
+                      const uint8_t *mask, int64_t mask_stride, const float *dlogp,
+                      const float *dentropy, const float *peak, const float *logz,
+                      const float *entropy, void *dlogits, int64_t dlogit_stride,
+                      uintptr_t stream);
+
+/* Gated feed-forward: h = act(x w[0]^T) * (x w[1]^T) for x [rows][D], w
+ * [2][H][D] (contiguous), h [rows][H], of type AV_BF16 or AV_F16 throughout.
+ * D, H and the row strides are multiples of 8, rows apart (a stride is at least
+ * the row's length), and the arrays 16-byte aligned: what TMA copies take.  act: AV_SILU, or AV_GELU (0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715
+ * g^3)))).  The products are exact and summed in 32 bits; h is rounded once. */
+enum { AV_SILU = 0, AV_GELU = 1 };
+int av_gated_ffn(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *x,
+                 int64_t x_stride, const void *w, void *h, int64_t h_stride, uintptr_t stream);
+
+/* Its gradient, dx [rows][D] and dw [2][H][D].  The projections are made
+ * again, so the forward pass keeps nothing; the gradients of the two
+ * projections are rounded to the arrays' type once, between the products. */
+int av_gated_ffn_grad(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *dh,
+                      int64_t dh_stride, const void *x, int64_t x_stride, const void *w, void *dx,
+                      int64_t dx_stride, void *dw, void *work, int64_t work_bytes,
+                      uintptr_t stream);
+int av_gated_ffn_work(int64_t rows, int64_t D, int64_t H, int64_t *bytes);
+
 /* Static description of a status code. */
 const char *av_strerror(int status);
 

@@ -25,7 +25,9 @@ RULE_BYTES = 408
 EXPORTS = ("av_create", "av_destroy", "av_reset", "av_set_state", "av_get_state", "av_step",
            "av_rollout", "av_expand", "av_search_init", "av_select", "av_select_static", "av_sync",
            "av_warnings", "av_rollout_path", "av_step_path", "av_observe", "av_rule_obs", "av_mutate", "av_set_variant", "av_strerror",
-           "av_last_error")
+           "av_last_error", "av_layer_norm", "av_layer_norm_grad", "av_layer_norm_work", "av_scan", "av_scan_grad",
+           "av_scan_sizes", "av_log_probs", "av_log_probs_grad", "av_gated_ffn", "av_gated_ffn_grad",
+           "av_gated_ffn_work")
 AV_MAX_WINDOW = 127
 AV_MAX_LIMIT = 255
 AV_PATH_VARIANT = 4
@@ -79,6 +81,7 @@ def load() -> ctypes.CDLL:
                            "`python -c 'import __graft_entry__ as g; g.build()'`")
     L = ctypes.CDLL(LIB_PATH)
     vp, i32, u64, up = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
+    i64, f32 = ctypes.c_int64, ctypes.c_float
     sig = {
         "av_create": [ctypes.POINTER(AvConfig), vp, ctypes.POINTER(vp)],
         "av_destroy": [vp],
@@ -100,6 +103,19 @@ def load() -> ctypes.CDLL:
         "av_rule_obs": [vp, vp, vp, up],
         "av_mutate": [i32, i32, i32, i32, i32, ctypes.POINTER(AvMutation), u64, vp, vp, up],
         "av_set_variant": [vp, ctypes.POINTER(AvVariant)],
+        # the policy operators: called by the functions of `policy`
+        "av_layer_norm": [i64, i32, i32, i32, f32, vp, i64, vp, vp, vp, i64, vp, vp, up],
+        "av_layer_norm_grad": [i64, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, up],
+        "av_layer_norm_work": [i64, i32, vp],
+        "av_scan": [i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, vp, i64, up],
+        "av_scan_grad": [i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, i64,
+                         i64, vp, i64, i64, vp, vp, i64, up],
+        "av_scan_sizes": [i64, i64, i64, i32, vp, vp],
+        "av_log_probs": [i64, i32, i32, vp, i64, vp, i32, vp, i64, i32, vp, vp, vp, vp, vp, vp, up],
+        "av_log_probs_grad": [i64, i32, i32, vp, i64, vp, i32, vp, i64, vp, vp, vp, vp, vp, vp, i64, up],
+        "av_gated_ffn": [i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, up],
+        "av_gated_ffn_grad": [i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, vp, i64, vp, vp, i64, up],
+        "av_gated_ffn_work": [i64, i64, i64, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)

@@ -12,10 +12,11 @@ SOURCES = [os.path.join(CSRC, f) for f in ("autoverse.cu", "k_fast_u8.cu", "k_fa
                                             "k_warp_u16.cu", "k_block.cu", "k_expand.cu", "k_search.cu",
                                             "k_observe.cu", "k_mutate.cu", "k_memo_u8.cu", "k_memo_u16.cu",
                                             "k_vmemo_u8.cu", "k_vmemo_u16.cu", "k_vmany_u8.cu", "k_vmany_u16.cu",
-                                            "k_variant.cu", "k_band.cu", "k_step.cu")]
+                                            "k_variant.cu", "k_band.cu", "k_step.cu", "policy.cu", "k_norm.cu",
+                                            "k_scan.cu", "k_logp.cu", "k_ffn.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "launch.h", "k_fast_impl.cuh", "k_warp_impl.cuh",
                                                      "k_memo_impl.cuh", "block_step.cuh", "small_step.cuh",
-                                                     "variant_keys.cuh")] + [
+                                                     "variant_keys.cuh", "policy.h", "values.cuh")] + [
     os.path.join(ROOT, "include", "autoverse.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

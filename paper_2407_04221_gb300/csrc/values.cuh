@@ -1,0 +1,34 @@
+// values.cuh -- the policy operators' value types: 32-bit floats, bf16, f16.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+namespace av {
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+
+template <class T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// Calls f with a value of the type that `dtype` names.
+template <class F>
+auto with_type(int dtype, F f)
+{
+    if (dtype == 1)
+        return f(__nv_bfloat16());
+    if (dtype == 2)
+        return f(__half());
+    return f(0.0f);
+}
+
+}  // namespace av
