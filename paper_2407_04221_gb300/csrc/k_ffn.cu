@@ -1,121 +1,809 @@
 // k_ffn.cu -- the gated feed-forward and its gradient.
 //   forward   g = x wg^T, u = x wu^T, h = act(g) u
 //   backward  dg = dh u act'(g), du = dh act(g); dx = dg wg + du wu; dwg = dg^T x, dwu = du^T x
+//
+// The products run on the tensor cores (tcgen05, accumulators in TMEM): one
+// persistent kernel in four forms, a pair of CTAs on a tile of 256 rows x 256
+// columns.  Per 64 terms a CTA fetches 128 rows of A and 128 of B (32 KB) for
+// 512 cycles of products; alone, a CTA on 128 x 256 would fetch 48 KB in the
+// same time, 96 bytes a cycle, more than an SM gets from L2.  In the forward
+// form the pair's 256 columns are 128 of the gate and 128 of the same columns
+// of the other projection, so one CTA's accumulators hold both factors of its
+// outputs and h leaves rounded once, with no array in between.  The backward
+// pass makes g and u again (4 M D H operations of 16) instead of keeping them:
+// kept in 16 bits they would cost accuracy, in 32 bits 8 bytes a unit.
+//
+// Warps: one issues copies (TMA), one products, four take accumulators to
+// memory while the next tile's products run (two sets of 256 TMEM columns).
+#include <cuda.h>
+
 #include "policy.h"
 #include "values.cuh"
 
 namespace av {
 namespace {
 
-constexpr int kTile = 16;
+// ------------------------------------------------------------ activations
 
-// act(g) and its slope
-__device__ __forceinline__ void activate(int act, float g, float &f, float &slope)
+// act(g) and its slope.  exp and the divide are the fast ones: good to 2^-21
+// relatively, a tenth of the outputs' rounding at most.
+template <int kAct>
+__device__ __forceinline__ void activate(float g, float &f, float &slope)
 {
-    if (act == AV_SILU) {
-        const float s = 1.0f / (1.0f + expf(-g));
-        f = g * s;
-        slope = s * (1.0f + g * (1.0f - s));
-    } else {
-        const float k = 0.7978845608028654f;  // sqrt(2 / pi)
-        const float t = tanhf(k * (g + 0.044715f * g * g * g));
-        f = 0.5f * g * (1.0f + t);
-        slope = 0.5f * (1.0f + t) + 0.5f * g * (1.0f - t * t) * k * (1.0f + 3.0f * 0.044715f * g * g);
-    }
+    // both are g times a sigmoid: of g, or of 2 sqrt(2/pi) (g + 0.044715 g^3)
+    const float c = 1.5957691216057308f, in = kAct == AV_SILU ? g : c * (g + 0.044715f * g * g * g);
+    const float s = __fdividef(1.0f, 1.0f + __expf(-in));
+    f = g * s;
+    const float din = kAct == AV_SILU ? 1.0f : c * (1.0f + 3.0f * 0.044715f * g * g);
+    slope = s + f * (1.0f - s) * din;
 }
 
-// A sum of products a(i, k) b(k, j) over k, 16 x 16 results a block.
-template <class A, class B>
-__device__ float tile_product(int64_t i, int64_t j, int64_t n, A a, B b, float (*sa)[kTile + 1], float (*sb)[kTile + 1])
-{
-    float sum = 0.0f;
-    for (int64_t k = 0; k < n; k += kTile) {
-        __syncthreads();
-        sa[threadIdx.y][threadIdx.x] = k + threadIdx.x < n ? a(i, k + threadIdx.x) : 0.0f;
-        sb[threadIdx.y][threadIdx.x] = k + threadIdx.y < n ? b(k + threadIdx.y, j) : 0.0f;
-        __syncthreads();
-        for (int q = 0; q < kTile; ++q)
-            sum += sa[threadIdx.y][q] * sb[q][threadIdx.x];
-    }
-    return sum;
-}
+// ------------------------------------------------------------ few rows
 
-// h, or with dh the projections' gradients dgu [rows][2][H].
+constexpr int kFewRows = 16;
+constexpr int kFewThreads = 256;
+
 template <class T>
-__global__ void ffn_kernel(int64_t rows, int64_t D, int64_t H, int act, const T *x, int64_t xs, const T *w, T *h,
-                           int64_t hs, const T *dh, int64_t dhs, T *dgu)
+__device__ __forceinline__ void unpack8(const uint4 &v, float *f)
 {
-    __shared__ float sa[kTile][kTile + 1], sb[kTile][kTile + 1];
-    const int64_t j = (int64_t)blockIdx.y * kTile + threadIdx.x, i = (int64_t)blockIdx.x * kTile + threadIdx.y;
-    auto xv = [&](int64_t r, int64_t k) { return r < rows ? to_f32(x[r * xs + k]) : 0.0f; };
-    const float g = tile_product(i, j, D, xv, [&](int64_t k, int64_t c) { return c < H ? to_f32(w[c * D + k]) : 0.0f; }, sa, sb);
-    const float u = tile_product(i, j, D, xv, [&](int64_t k, int64_t c) { return c < H ? to_f32(w[(H + c) * D + k]) : 0.0f; }, sa, sb);
-    if (i >= rows || j >= H)
+    const T *p = reinterpret_cast<const T *>(&v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        f[i] = to_f32(p[i]);
+}
+
+// A warp per unit of H: its two rows of weights stream past, 16 bytes a lane,
+// against R rows of x that stay in L1.  Bound by the weights' bytes.
+template <class T, int kAct, int R, bool kGrad>
+__global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t D, int64_t H, const T *x, int64_t xs,
+                                                               const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
+                                                               T *dgu)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t j = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
+    if (j >= H)
         return;
-    float f, slope;
-    activate(act, g, f, slope);
-    if (h)
-        h[i * hs + j] = from_f32<T>(f * u);
-    if (dh) {
-        const float d = to_f32(dh[i * dhs + j]);
-        dgu[i * 2 * H + j] = from_f32<T>(d * u * slope);
-        dgu[i * 2 * H + H + j] = from_f32<T>(d * f);
+    const T *wg = w + j * D, *wu = w + (H + j) * D;
+    float g[R] = {}, u[R] = {};
+#pragma unroll 2
+    for (int64_t k = lane * 8; k < D; k += 256) {
+        float a[8], b[8];
+        unpack8<T>(__ldg(reinterpret_cast<const uint4 *>(wg + k)), a);
+        unpack8<T>(__ldg(reinterpret_cast<const uint4 *>(wu + k)), b);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r >= rows)
+                break;
+            float v[8];
+            unpack8<T>(__ldg(reinterpret_cast<const uint4 *>(x + r * xs + k)), v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                g[r] += v[i] * a[i];
+                u[r] += v[i] * b[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            g[r] += __shfl_xor_sync(~0u, g[r], o);
+            u[r] += __shfl_xor_sync(~0u, u[r], o);
+        }
+        if (lane != r || r >= rows)
+            continue;
+        float f, slope;
+        activate<kAct>(g[r], f, slope);
+        if (!kGrad) {
+            h[r * hs + j] = from_f32<T>(f * u[r]);
+        } else {
+            const float d = to_f32(dh[r * dhs + j]);
+            dgu[r * 2 * H + j] = from_f32<T>(d * u[r] * slope);
+            dgu[r * 2 * H + H + j] = from_f32<T>(d * f);
+        }
     }
 }
 
-template <class T>
-__global__ void ffn_dx_kernel(int64_t rows, int64_t D, int64_t H, const T *dgu, const T *w, T *dx, int64_t dxs)
+// ------------------------------------------------------------ products
+
+constexpr int kRowsCta = 128;  // accumulator rows of a CTA, and B rows it fetches
+constexpr int kTile = 256;     // rows and columns of a pair's tile
+constexpr int kBlockK = 64;    // terms a stage: 128 bytes, the swizzle's width
+constexpr int kHalf = kRowsCta * kBlockK * 2;  // bytes of A or of B a CTA fetches per stage
+constexpr int kStages = 6;
+constexpr int kSlab = kRowsCta * 128;  // staging of 128 rows x 128 bytes on the way out
+constexpr int kSmem = kStages * 2 * kHalf + 2 * kSlab + 1024 + 256;
+constexpr int kThreads = 192;
+constexpr int kTmemCols = 512;
+
+enum Form {
+    kForward,  // h
+    kProjGrad, // dg, du from dh and the projections made again
+    kTimesW,   // dx = dgu w: B runs along its rows
+    kTransposed // dw = dgu^T x: A and B run along their rows
+};
+
+struct Params {
+    int m, n;               // rows and columns of the result (forward forms: columns of H)
+    int m_tiles, n_tiles;   // of a pair
+    int k_blocks, splits;   // blocks of 64 terms in all, parts that they are dealt to
+    const void *dh;
+    int64_t dhs;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ uint32_t cta_rank()
 {
-    __shared__ float sa[kTile][kTile + 1], sb[kTile][kTile + 1];
-    const int64_t j = (int64_t)blockIdx.y * kTile + threadIdx.x, i = (int64_t)blockIdx.x * kTile + threadIdx.y;
-    const float v = tile_product(i, j, 2 * H, [&](int64_t r, int64_t k) { return r < rows ? to_f32(dgu[r * 2 * H + k]) : 0.0f; },
-                                 [&](int64_t k, int64_t c) { return c < D ? to_f32(w[k * D + c]) : 0.0f; }, sa, sb);
-    if (i < rows && j < D)
-        dx[i * dxs + j] = from_f32<T>(v);
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ uint64_t now_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+
+constexpr uint64_t kGiveUpNs = 4000000000ull;
+
+// Waits for the barrier's phase; false after some seconds, or at once when the
+// block has given up elsewhere.
+__device__ bool bar_wait(uint32_t bar, uint32_t phase, volatile int *dead)
+{
+    uint64_t began = 0;
+    for (uint32_t spins = 0;; ++spins) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                     "selp.b32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(phase)
+                     : "memory");
+        if (done)
+            return true;
+        if ((spins & 63) != 63)
+            continue;
+        if (*dead)
+            return false;
+        const uint64_t t = now_ns();
+        if (!began)
+            began = t;
+        else if (t - began > kGiveUpNs) {
+            *dead = 1;
+            return false;
+        }
+    }
+}
+
+// A box of a tensor map to this CTA's shared memory; the bytes are counted at
+// a barrier of the pair's first CTA.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map),
+                 "r"(src), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+
+// Closes a group of stores, which may be empty: slabs are counted by groups.
+__device__ __forceinline__ void stores_close() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+
+template <int N>
+__device__ __forceinline__ void stores_left()
+{
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+
+// Shared-memory operand, 128-byte swizzle.  Along its terms (K-major): rows of
+// 128 bytes, groups of eight rows 1024 bytes apart.  Along its rows
+// (MN-major): boxes of 64 rows x 64 terms, a term's 64 rows in 128 bytes,
+// groups of eight terms 1024 bytes apart, the next 64 rows 8192 bytes on.
+template <bool kAlongRows>
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
+{
+    const uint64_t lead = kAlongRows ? 8192 >> 4 : 1, group = 1024 >> 4;
+    return (uint64_t)(addr >> 4 & 0x3fff) | lead << 16 | group << 32 | 1ull << 46 | 2ull << 61;
+}
+
+__device__ __forceinline__ void multiply(uint32_t acc, uint64_t a, uint64_t b, uint32_t kind, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(acc),
+                 "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add)
+                 : "memory");
+}
+
+// The barrier, in both CTAs, when all products issued so far are done.
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+
+// 32 columns of this thread's accumulator row.
+__device__ __forceinline__ void load_acc(uint32_t addr, float (&v)[32])
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]),
+                   "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+                   "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]),
+                   "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr));
+}
+
+__device__ __forceinline__ void wait_acc() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    T v[2] = {from_f32<T>(a), from_f32<T>(b)};
+    return *reinterpret_cast<uint32_t *>(v);
+}
+
+// 16 bytes of a row into a staging slab, in the 128-byte swizzle.
+__device__ __forceinline__ void put16(uint32_t slab, int row, int chunk, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    const uint32_t at = slab + row * 128 + ((chunk ^ (row & 7)) << 4);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 template <class T>
-__global__ void ffn_dw_kernel(int64_t rows, int64_t D, int64_t H, const T *dgu, const T *x, int64_t xs, T *dw)
+__device__ __forceinline__ void put32(uint32_t slab, int row, int half, const float (&v)[32])
 {
-    __shared__ float sa[kTile][kTile + 1], sb[kTile][kTile + 1];
-    const int64_t j = (int64_t)blockIdx.y * kTile + threadIdx.x, i = (int64_t)blockIdx.x * kTile + threadIdx.y;
-    const float v = tile_product(i, j, rows, [&](int64_t c, int64_t r) { return c < 2 * H ? to_f32(dgu[r * 2 * H + c]) : 0.0f; },
-                                 [&](int64_t r, int64_t c) { return c < D ? to_f32(x[r * xs + c]) : 0.0f; }, sa, sb);
-    if (i < 2 * H && j < D)
-        dw[i * D + j] = from_f32<T>(v);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        put16(slab, row, half * 4 + c, pack2<T>(v[8 * c], v[8 * c + 1]), pack2<T>(v[8 * c + 2], v[8 * c + 3]),
+              pack2<T>(v[8 * c + 4], v[8 * c + 5]), pack2<T>(v[8 * c + 6], v[8 * c + 7]));
 }
 
-dim3 grid_of(int64_t rows, int64_t cols) { return dim3((unsigned)((rows + kTile - 1) / kTile), (unsigned)((cols + kTile - 1) / kTile)); }
+__device__ __forceinline__ void epilogue_sync()
+{
+    __syncwarp();
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+struct Tile {
+    int m, n, k0, k1, split;
+};
+
+// Tiles in bands of eight rows of tiles, down the band first: those in flight
+// together share A and B in L2.
+__device__ __forceinline__ Tile tile_of(const Params &p, int i)
+{
+    const int per = p.m_tiles * p.n_tiles;
+    Tile t;
+    t.split = i / per;
+    i -= t.split * per;
+    const int band = i / (8 * p.n_tiles), first = band * 8;
+    const int high = min(8, p.m_tiles - first);
+    const int at = i - band * 8 * p.n_tiles;
+    t.m = first + at % high;
+    t.n = at / high;
+    t.k0 = (int)((int64_t)p.k_blocks * t.split / p.splits);
+    t.k1 = (int)((int64_t)p.k_blocks * (t.split + 1) / p.splits);
+    return t;
+}
+
+template <class T, int kForm, int kAct, bool kParts>
+__global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_kernel(
+    const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+    const __grid_constant__ CUtensorMap out_map, const Params p)
+{
+    constexpr bool kARows = kForm == kTransposed, kBRows = kForm == kTimesW || kForm == kTransposed;
+    constexpr bool kGated = kForm == kForward || kForm == kProjGrad;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t slabs = base + kStages * 2 * kHalf;
+    const uint32_t bars = slabs + 2 * kSlab;
+    // barriers: full[stage], empty[stage], acc_full[2], acc_empty[2]
+    const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16;
+    uint8_t *tail = raw + (bars + 16 * kStages + 32 - smem_addr(raw));
+    volatile int *dead = reinterpret_cast<volatile int *>(tail);
+    uint32_t *tmem_at = reinterpret_cast<uint32_t *>(tail) + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cta_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int tiles = p.m_tiles * p.n_tiles * p.splits;
+
+    if (threadIdx.x == 0) {
+        *dead = 0;
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full + 8 * s, 1);
+            bar_init(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            bar_init(acc_full + 8 * s, 1);
+            bar_init(acc_empty + 8 * s, 8);  // four warps in either CTA
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_at)),
+                     "r"(kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tmem_at);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int step = 0;
+            bool ok = true;
+            for (int i = pair; ok && i < tiles; i += pairs) {
+                const Tile t = tile_of(p, i);
+                const int am = t.m * kTile + rank * kRowsCta;  // this CTA's rows of A
+                // its rows of B: of the gate (first CTA) or the other projection (second), or half the tile's columns
+                const int bn = kGated ? t.n * kRowsCta + (int)rank * p.n : t.n * kTile + (int)rank * kRowsCta;
+                for (int k = t.k0; k < t.k1; ++k, ++step) {
+                    const int s = step % kStages;
+                    if (!(ok = bar_wait(empty + 8 * s, (step / kStages & 1) ^ 1, dead)))
+                        break;
+                    if (rank == 0)
+                        bar_expect(full + 8 * s, 4 * kHalf);
+                    const uint32_t bar = in_cta(full + 8 * s, 0), a = base + s * 2 * kHalf, b = a + kHalf;
+                    if (kARows) {
+                        load_box(a, &a_map, am, k * kBlockK, bar);
+                        load_box(a + kHalf / 2, &a_map, am + 64, k * kBlockK, bar);
+                    } else {
+                        load_box(a, &a_map, k * kBlockK, am, bar);
+                    }
+                    if (kBRows) {
+                        load_box(b, &b_map, bn, k * kBlockK, bar);
+                        load_box(b + kHalf / 2, &b_map, bn + 64, k * kBlockK, bar);
+                    } else {
+                        load_box(b, &b_map, k * kBlockK, bn, bar);
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            // 32-bit sums, operands bf16 or f16, 256 x 256, each along its terms or its rows
+            const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            const uint32_t kind = 1u << 4 | type << 7 | type << 10 | (uint32_t)kARows << 15 | (uint32_t)kBRows << 16 |
+                                  (kTile / 8) << 17 | (kTile / 16) << 24;
+            int step = 0, done = 0;
+            bool ok = true;
+            for (int i = pair; ok && i < tiles; i += pairs, ++done) {
+                const Tile t = tile_of(p, i);
+                const int set = done & 1;
+                if (!(ok = bar_wait(acc_empty + 8 * set, (done >> 1 & 1) ^ 1, dead)))
+                    break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t acc = tmem + set * kTile;
+                for (int k = t.k0; k < t.k1; ++k, ++step) {
+                    const int s = step % kStages;
+                    if (!(ok = bar_wait(full + 8 * s, step / kStages & 1, dead)))
+                        break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = base + s * 2 * kHalf;
+                    const uint64_t a = operand<kARows>(at), b = operand<kBRows>(at + kHalf);
+#pragma unroll
+                    for (int q = 0; q < kBlockK / 16; ++q)  // 16 terms: 32 bytes on, or two groups of eight terms
+                        multiply(acc, a + q * (kARows ? 128 : 2), b + q * (kBRows ? 128 : 2), kind, k > t.k0 || q > 0);
+                    commit(empty + 8 * s);
+                }
+                if (ok)
+                    commit(acc_full + 8 * set);
+            }
+        }
+    } else {
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        const bool first = threadIdx.x == 64;
+        int done = 0;
+        for (int i = pair; i < tiles; i += pairs, ++done) {
+            const Tile t = tile_of(p, i);
+            const int set = done & 1;
+            // (past a wait that ran out the outputs are NaN, so that no wrong result passes for a right one)
+            const bool ok = __all_sync(~0u, bar_wait(acc_full + 8 * set, done >> 1 & 1, dead));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + set * kTile + ((uint32_t)(quarter * 32) << 16);
+            const int m0 = t.m * kTile + rank * kRowsCta;
+            auto columns = [&](int c, float (&v)[32]) {
+                if (ok) {
+                    load_acc(acc + c, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        v[e] = __int_as_float(0x7fffffff);
+                }
+            };
+            if (kGated) {
+#pragma unroll 1
+                for (int c = 0; c < kRowsCta; c += 64) {  // 64 columns of H
+                    if (first) {
+                        if (kForm == kForward)
+                            stores_left<1>();
+                        else
+                            stores_left<0>();
+                    }
+                    epilogue_sync();
+                    const uint32_t slab = slabs + (kForm == kForward ? (c >> 6) * kSlab : 0);
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        float g[32], u[32];
+                        columns(c + half * 32, g);
+                        columns(kRowsCta + c + half * 32, u);
+                        const int col = t.n * kRowsCta + c + half * 32;
+                        if (kForm == kForward) {
+                            wait_acc();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                float f, slope;
+                                activate<kAct>(g[e], f, slope);
+                                g[e] = f * u[e];
+                            }
+                            put32<T>(slab, row, half, g);
+                        } else {
+                            const T *dh = (const T *)p.dh + (int64_t)(m0 + row) * p.dhs + col;
+                            float d[32];
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) {
+                                uint4 q = make_uint4(0, 0, 0, 0);
+                                if (m0 + row < p.m && col + e < p.n)
+                                    q = __ldg(reinterpret_cast<const uint4 *>(dh + e));
+                                unpack8<T>(q, d + e);
+                            }
+                            wait_acc();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                float f, slope;
+                                activate<kAct>(g[e], f, slope);
+                                g[e] = d[e] * u[e] * slope;
+                                u[e] = d[e] * f;
+                            }
+                            put32<T>(slab, row, half, g);
+                            put32<T>(slab + kSlab, row, half, u);
+                        }
+                    }
+                    fence_async();
+                    epilogue_sync();
+                    if (first && t.n * kRowsCta + c < p.n && m0 < p.m) {
+                        const int col = t.n * kRowsCta + c;
+                        store_box(&out_map, slab, col, 0, m0);
+                        if (kForm == kProjGrad)
+                            store_box(&out_map, slab + kSlab, col, 1, m0);
+                    }
+                    if (first)
+                        stores_close();
+                }
+            } else {
+                constexpr int kWide = kParts ? 32 : 64;  // columns of 128 bytes
+#pragma unroll 1
+                for (int c = 0; c < kTile; c += kWide) {
+                    if (first)
+                        stores_left<1>();
+                    epilogue_sync();
+                    const uint32_t slab = slabs + (c / kWide & 1) * kSlab;
+                    float v[32];
+                    if (kParts) {
+                        columns(c, v);
+                        wait_acc();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            put16(slab, row, q, __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                                  __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+                    } else {
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            columns(c + half * 32, v);
+                            wait_acc();
+                            put32<T>(slab, row, half, v);
+                        }
+                    }
+                    fence_async();
+                    epilogue_sync();
+                    if (first && t.n * kTile + c < p.n && m0 < p.m)
+                        store_box(&out_map, slab, t.n * kTile + c, m0, t.split);
+                    if (first)
+                        stores_close();
+                }
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0)
+                bar_arrive_cluster(in_cta(acc_empty + 8 * set, 0));
+        }
+        if (first)
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    __syncthreads();
+    if (*dead) {  // copies and products may still be under way: leave them some time
+        const uint64_t began = now_ns();
+        while (now_ns() - began < 10000000ull) {
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster_sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
+}
+
+// The sum of the parts, rounded; parts in order.
+template <class T>
+__global__ void ffn_parts_kernel(int64_t rows, int64_t cols, int splits, const float *parts, T *out, int64_t os)
+{
+    const int64_t per = cols / 4, n = rows * per;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+        float4 v = reinterpret_cast<const float4 *>(parts)[i];
+        for (int s = 1; s < splits; ++s) {
+            const float4 q = reinterpret_cast<const float4 *>(parts)[i + s * n];
+            v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+        }
+        *reinterpret_cast<uint2 *>(out + i / per * os + i % per * 4) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
+    }
+}
+
+// ------------------------------------------------------------ host
+
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                            const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                            CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder()
+{
+    static const Encode fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) !=
+                cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            return (Encode) nullptr;
+        return (Encode)p;
+    }();
+    return fn;
+}
+
+// dims, box: innermost first; strides of the outer dims in elements.
+bool make_map(CUtensorMap *map, int dtype, const void *p, int rank, const int64_t *dims, const int64_t *strides,
+              const int *box)
+{
+    const int64_t e = dtype == AV_F32 ? 4 : 2;
+    cuuint64_t d[3], s[2];
+    cuuint32_t b[3], one[3] = {1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        d[i] = (cuuint64_t)dims[i];
+        b[i] = (cuuint32_t)box[i];
+        if (i > 0)
+            s[i - 1] = (cuuint64_t)(strides[i - 1] * e);
+    }
+    const CUtensorMapDataType type = dtype == AV_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                     : dtype == AV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return encoder()(map, type, (cuuint32_t)rank, const_cast<void *>(p), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// An operand: [rows][cols], boxes of box_rows x 64 columns.
+bool operand_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64_t cols, int64_t stride, int box_rows)
+{
+    const int64_t dims[2] = {cols, rows}, strides[1] = {rows > 1 ? stride : cols};
+    const int box[2] = {64, box_rows};
+    return make_map(map, dtype, p, 2, dims, strides, box);
+}
+
+constexpr int kPairs = 76;  // of a GB300's 152 SMs
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Into how many parts the terms of a product are dealt: the number that ends
+// soonest.  A block of 64 terms takes a pair 0.27 us; each part writes its
+// sums in 32 bits, 0.8 us a tile, and a pass adds them up (3 us and 8 bytes a
+// sum and part at 5 TB/s).
+int splits_for(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t tiles = up(m, kTile) * up(n, kTile), blocks = up(k, kBlockK);
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s <= 16 && s <= blocks; ++s) {
+        const double waves = (double)up(tiles * s, kPairs), length = (double)up(blocks, s);
+        double us = waves * (0.27 * length + (s > 1 ? 0.8 : 0.4));
+        if (s > 1)
+            us += 3.0 + (double)m * n * 8 * s / 5e6;
+        if (s == 1 || us < least) {
+            least = us;
+            best = s;
+        }
+    }
+    return best;
+}
+
+int64_t parts_bytes(int64_t m, int64_t n, int64_t k)
+{
+    const int s = splits_for(m, n, k);
+    return s > 1 ? (int64_t)s * m * n * 4 : 0;
+}
+
+int64_t dgu_bytes(int64_t rows, int64_t H) { return up(rows * 2 * H * 2, 256) * 256; }
+
+template <class T, int kForm, int kAct, bool kParts>
+cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Params &p, cudaStream_t st)
+{
+    const auto kernel = ffn_kernel<T, kForm, kAct, kParts>;  // (kAct plays no part in the last two forms)
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess)
+        return e;
+    const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles * p.splits;
+    kernel<<<2 * (unsigned)(tiles < kPairs ? tiles : kPairs), kThreads, kSmem, st>>>(a, b, out, p);
+    return cudaGetLastError();
+}
+
+// out [m][n] = A B, in one go or in parts.
+template <class T, int kForm>
+cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64_t m, int64_t n, int64_t k, void *out,
+                    int64_t os, float *parts, cudaStream_t st)
+{
+    Params p{};
+    p.m = (int)m;
+    p.n = (int)n;
+    p.m_tiles = (int)up(m, kTile);
+    p.n_tiles = (int)up(n, kTile);
+    p.k_blocks = (int)up(k, kBlockK);
+    p.splits = splits_for(m, n, k);
+    CUtensorMap map;
+    const int64_t dims[3] = {n, m, p.splits};
+    if (p.splits == 1) {
+        const int64_t strides[2] = {m > 1 ? os : n, (m > 1 ? os : n) * m};
+        const int box[3] = {64, kRowsCta, 1};
+        if (!make_map(&map, dtype, out, 3, dims, strides, box))
+            return cudaErrorInvalidValue;
+        return go<T, kForm, AV_SILU, false>(a, b, map, p, st);
+    }
+    const int64_t strides[2] = {n, m * n};
+    const int box[3] = {32, kRowsCta, 1};
+    if (!make_map(&map, AV_F32, parts, 3, dims, strides, box))
+        return cudaErrorInvalidValue;
+    cudaError_t e = go<T, kForm, AV_SILU, true>(a, b, map, p, st);
+    if (e != cudaSuccess)
+        return e;
+    const int64_t blocks = up(m * n / 4, 256);
+    ffn_parts_kernel<T><<<(unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 256, 0, st>>>(m, n, p.splits, parts, (T *)out,
+                                                                                      m > 1 ? os : n);
+    return cudaGetLastError();
+}
+
+template <class T, int kAct, bool kGrad>
+void few(int rows, int64_t D, int64_t H, const T *x, int64_t xs, const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
+         T *dgu, cudaStream_t st)
+{
+    const unsigned grid = (unsigned)up(H, kFewThreads / 32);
+    if (rows <= 1)
+        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+    else if (rows <= 4)
+        ffn_few_kernel<T, kAct, 4, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+    else
+        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+}
+
+// h, or the projections' gradients [rows][2][H].
+template <class T, int kAct, bool kGrad>
+cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, int64_t xs, const void *w, void *h,
+                  int64_t hs, const void *dh, int64_t dhs, void *dgu, cudaStream_t st)
+{
+    if (rows <= kFewRows) {
+        few<T, kAct, kGrad>((int)rows, D, H, (const T *)x, xs, (const T *)w, (T *)h, hs, (const T *)dh, dhs, (T *)dgu,
+                            st);
+        return cudaGetLastError();
+    }
+    Params p{};
+    p.m = (int)rows;
+    p.n = (int)H;
+    p.m_tiles = (int)up(rows, kTile);
+    p.n_tiles = (int)up(H, kRowsCta);
+    p.k_blocks = (int)up(D, kBlockK);
+    p.splits = 1;
+    p.dh = dh;
+    p.dhs = dhs;
+    CUtensorMap a, b, out;
+    // (stores are columns, projection, row; h has one)
+    const int64_t dims[3] = {H, kGrad ? 2 : 1, rows}, strides[2] = {H, kGrad ? 2 * H : hs};
+    const int box[3] = {64, 1, kRowsCta};
+    if (!operand_map(&a, dtype, x, rows, D, xs, kRowsCta) || !operand_map(&b, dtype, w, 2 * H, D, D, kRowsCta) ||
+        !make_map(&out, dtype, kGrad ? dgu : h, 3, dims, strides, box))
+        return cudaErrorInvalidValue;
+    return go<T, kGrad ? kProjGrad : kForward, kAct, false>(a, b, out, p, st);
+}
 
 }  // namespace
 
-int64_t ffn_work_bytes(int64_t rows, int64_t, int64_t H) { return rows * 2 * H * 2; }
+int64_t ffn_work_bytes(int64_t rows, int64_t D, int64_t H)
+{
+    const int64_t a = parts_bytes(rows, D, 2 * H), b = parts_bytes(2 * H, D, rows);
+    return dgu_bytes(rows, H) + (a > b ? a : b);
+}
 
 cudaError_t launch_ffn(int64_t rows, int64_t D, int64_t H, int dtype, int act, const void *x, int64_t x_stride,
                        const void *w, void *h, int64_t h_stride, cudaStream_t st)
 {
-    with_type(dtype, [&](auto v) {
+    if (!encoder())
+        return cudaErrorNotSupported;
+    auto run = [&](auto v) {
         using T = decltype(v);
-        ffn_kernel<T><<<grid_of(rows, H), dim3(kTile, kTile), 0, st>>>(rows, D, H, act, (const T *)x, x_stride, (const T *)w,
-                                                                (T *)h, h_stride, nullptr, 0, nullptr);
-    });
-    return cudaGetLastError();
+        return act == AV_SILU ? gated<T, AV_SILU, false>(dtype, rows, D, H, x, x_stride, w, h, h_stride, nullptr, 0,
+                                                         nullptr, st)
+                              : gated<T, AV_GELU, false>(dtype, rows, D, H, x, x_stride, w, h, h_stride, nullptr, 0,
+                                                         nullptr, st);
+    };
+    return dtype == AV_BF16 ? run(__nv_bfloat16()) : run(__half());
 }
 
 cudaError_t launch_ffn_grad(int64_t rows, int64_t D, int64_t H, int dtype, int act, const void *dh, int64_t dh_stride,
                             const void *x, int64_t x_stride, const void *w, void *dx, int64_t dx_stride, void *dw,
                             void *work, cudaStream_t st)
 {
-    with_type(dtype, [&](auto v) {
+    if (!encoder())
+        return cudaErrorNotSupported;
+    float *parts = reinterpret_cast<float *>((char *)work + dgu_bytes(rows, H));
+    auto run = [&](auto v) {
         using T = decltype(v);
-        ffn_kernel<T><<<grid_of(rows, H), dim3(kTile, kTile), 0, st>>>(rows, D, H, act, (const T *)x, x_stride, (const T *)w,
-                                                                nullptr, 0, (const T *)dh, dh_stride, (T *)work);
-        ffn_dx_kernel<T><<<grid_of(rows, D), dim3(kTile, kTile), 0, st>>>(rows, D, H, (const T *)work, (const T *)w, (T *)dx,
-                                                                   dx_stride);
-        ffn_dw_kernel<T><<<grid_of(2 * H, D), dim3(kTile, kTile), 0, st>>>(rows, D, H, (const T *)work, (const T *)x,
-                                                                    x_stride, (T *)dw);
-    });
-    return cudaGetLastError();
+        cudaError_t e = act == AV_SILU ? gated<T, AV_SILU, true>(dtype, rows, D, H, x, x_stride, w, nullptr, 0, dh,
+                                                                 dh_stride, work, st)
+                                       : gated<T, AV_GELU, true>(dtype, rows, D, H, x, x_stride, w, nullptr, 0, dh,
+                                                                 dh_stride, work, st);
+        if (e != cudaSuccess)
+            return e;
+        CUtensorMap dgu, wt, dgut, xt;
+        if (!operand_map(&dgu, dtype, work, rows, 2 * H, 2 * H, kRowsCta) || !operand_map(&wt, dtype, w, 2 * H, D, D, 64) ||
+            !operand_map(&dgut, dtype, work, rows, 2 * H, 2 * H, 64) || !operand_map(&xt, dtype, x, rows, D, x_stride, 64))
+            return cudaErrorInvalidValue;
+        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, st);
+        if (e != cudaSuccess)
+            return e;
+        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, st);
+    };
+    return dtype == AV_BF16 ? run(__nv_bfloat16()) : run(__half());
 }
 
 }  // namespace av
