@@ -23,6 +23,9 @@ import torch
 
 from . import AvError, _stream, av_strerror, load
 
+# the current stream's handle by device index: 0.1 us, where making a Stream object takes 2.9
+_current = torch._C._cuda_getCurrentRawStream
+
 AV_F32, AV_BF16, AV_F16 = 0, 1, 2
 AV_SILU, AV_GELU = 0, 1
 MAX_TOP = 32
@@ -141,11 +144,11 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     w = _dense("weight", weight, x, None, (n,))
     b = _dense("bias", bias, x, None if param is None else param.dtype, (n,))
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
-    at = stats.data_ptr()
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     _check("av_layer_norm", load().av_layer_norm(rows, n, dtype, pt, eps, x.data_ptr(), stride, w, b, y.data_ptr(), n,
-                                                 at, at + 4 * rows, _stream(None)))
-    return y, stats[0], stats[1]
+                                                 mean.data_ptr(), rstd.data_ptr(), _current(x.get_device())))
+    return y, mean, rstd
 
 
 @_on_stream
@@ -163,11 +166,12 @@ def layer_norm_grad(dy, x, weight, mean, rstd):
     need = ctypes.c_int64()
     _check("av_layer_norm_work", L.av_layer_norm_work(rows, n, ctypes.byref(need)))
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw, db = torch.empty((2, n), dtype=torch.float32 if weight is None else weight.dtype, device=x.device)
+    dw = torch.empty(n, dtype=torch.float32 if weight is None else weight.dtype, device=x.device)
+    db = torch.empty_like(dw)
     work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
     _check("av_layer_norm_grad", L.av_layer_norm_grad(
         rows, n, dtype, pt, dy.data_ptr(), _rows("dy", dy)[2], x.data_ptr(), stride, w, m, r, dx.data_ptr(), n,
-        dw.data_ptr(), db.data_ptr(), work.data_ptr(), need.value, _stream(None)))
+        dw.data_ptr(), db.data_ptr(), work.data_ptr(), need.value, _current(x.get_device())))
     return dx, dw, db
 
 
@@ -208,7 +212,7 @@ def scan(gate, value, reset=None, h0=None, save=False):
     work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _check("av_scan", load().av_scan(T, B, D, dtype, *where, first, h.data_ptr(), B * D, D, last.data_ptr(),
                                      states.data_ptr() if save else None, work.data_ptr() if need else None, need,
-                                     _stream(None)))
+                                     _current(gate.get_device())))
     return (h, last, states) if save else (h, last)
 
 
@@ -227,7 +231,8 @@ def scan_grad(dh, gate, value, reset, states, dlast=None):
     work = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _check("av_scan_grad", load().av_scan_grad(
         T, B, D, dtype, dh.data_ptr(), *_seq("dh", dh), *where, state, last, dgate.data_ptr(), B * D, D,
-        dvalue.data_ptr(), B * D, D, dh0.data_ptr(), work.data_ptr() if need else None, need, _stream(None)))
+        dvalue.data_ptr(), B * D, D, dh0.data_ptr(), work.data_ptr() if need else None, need,
+        _current(gate.get_device())))
     return dgate, dvalue, dh0
 
 
@@ -268,16 +273,15 @@ def log_probs(logits, tokens, mask=None, top=0):
     if not 0 <= top <= min(V, MAX_TOP):
         raise ValueError(f"top: expected 0..{min(V, MAX_TOP)}")
     lead, dev = logits.shape[:-1], logits.device
-    stats = torch.empty((4, *lead), dtype=torch.float32, device=dev)
-    out = dict(zip(("logp", "entropy", "peak", "logz"), stats.unbind(0)))
+    out = {k: torch.empty(lead, dtype=torch.float32, device=dev) for k in ("logp", "entropy", "peak", "logz")}
     values = index = None
     if top:
         out["top_logp"] = torch.empty((*lead, top), dtype=torch.float32, device=dev)
         out["top_index"] = torch.empty((*lead, top), dtype=torch.int32, device=dev)
         values, index = out["top_logp"].data_ptr(), out["top_index"].data_ptr()
-    at = stats.data_ptr()
-    _check("av_log_probs", load().av_log_probs(*where, top, at, at + 4 * rows, at + 8 * rows, at + 12 * rows, values,
-                                               index, _stream(None)))
+    _check("av_log_probs", load().av_log_probs(
+        *where, top, out["logp"].data_ptr(), out["entropy"].data_ptr(), out["peak"].data_ptr(), out["logz"].data_ptr(),
+        values, index, _current(logits.get_device())))
     return out
 
 
@@ -291,7 +295,8 @@ def log_probs_grad(dlogp, dentropy, logits, tokens, out, mask=None):
                           (("dlogp", dlogp), ("dentropy", dentropy), ("peak", out["peak"]), ("logz", out["logz"]),
                            ("entropy", out["entropy"])))
     dx = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _check("av_log_probs_grad", load().av_log_probs_grad(*where, dl, de, pk, lz, en, dx.data_ptr(), V, _stream(None)))
+    _check("av_log_probs_grad", load().av_log_probs_grad(*where, dl, de, pk, lz, en, dx.data_ptr(), V,
+                                                         _current(logits.get_device())))
     return dx
 
 
@@ -316,7 +321,7 @@ def gated_ffn(x, w, act="silu"):
     rows, D, H, dtype, a, stride = _ffn_inputs(x, w, act)
     h = torch.empty((*x.shape[:-1], H), dtype=x.dtype, device=x.device)
     _check("av_gated_ffn", load().av_gated_ffn(rows, D, H, dtype, a, x.data_ptr(), stride, w.data_ptr(), h.data_ptr(),
-                                               H, _stream(None)))
+                                               H, _current(x.get_device())))
     return h
 
 
@@ -333,5 +338,6 @@ def gated_ffn_grad(dh, x, w, act="silu"):
     work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
     _check("av_gated_ffn_grad", L.av_gated_ffn_grad(rows, D, H, dtype, a, dh.data_ptr(), _rows("dh", dh)[2],
                                                     x.data_ptr(), stride, w.data_ptr(), dx.data_ptr(), D,
-                                                    dw.data_ptr(), work.data_ptr(), need.value, _stream(None)))
+                                                    dw.data_ptr(), work.data_ptr(), need.value,
+                                                    _current(x.get_device())))
     return dx, dw
