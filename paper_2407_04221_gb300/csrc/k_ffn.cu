@@ -17,6 +17,7 @@
 // memory while the next tile's products run (two sets of 256 TMEM columns).
 #include <cuda.h>
 
+#include "async.cuh"
 #include "policy.h"
 #include "values.cuh"
 
@@ -131,8 +132,6 @@ struct Params {
     int64_t dhs;
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
 __device__ __forceinline__ uint32_t cta_rank()
 {
     uint32_t r;
@@ -152,57 +151,9 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
-__device__ __forceinline__ uint64_t now_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-
-constexpr uint64_t kGiveUpNs = 4000000000ull;
-
-// Waits for the barrier's phase; false after some seconds, or at once when the
-// block has given up elsewhere.
-__device__ bool bar_wait(uint32_t bar, uint32_t phase, volatile int *dead)
-{
-    uint64_t began = 0;
-    for (uint32_t spins = 0;; ++spins) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\t"
-                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-                     "selp.b32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done)
-                     : "r"(bar), "r"(phase)
-                     : "memory");
-        if (done)
-            return true;
-        if ((spins & 63) != 63)
-            continue;
-        if (*dead)
-            return false;
-        const uint64_t t = now_ns();
-        if (!began)
-            began = t;
-        else if (t - began > kGiveUpNs) {
-            *dead = 1;
-            return false;
-        }
-    }
 }
 
 // A box of a tensor map to this CTA's shared memory; the bytes are counted at
@@ -558,11 +509,8 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
     }
     __syncwarp();
     __syncthreads();
-    if (*dead) {  // copies and products may still be under way: leave them some time
-        const uint64_t began = now_ns();
-        while (now_ns() - began < 10000000ull) {
-        }
-    }
+    if (*dead)  // copies and products may still be under way
+        linger();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");

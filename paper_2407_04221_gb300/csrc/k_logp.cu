@@ -3,18 +3,22 @@
 //   logz = log sum e,  log p_j = (x_j - m) - logz,  entropy = logz - sum e (x - m) / sum e
 //   dx_j = dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy)
 //
-// Forward, the logits are read once: every thread keeps a running maximum with
-// the sums below it, brought to a new maximum when one comes, and the threads'
-// sums are joined at the row's.  Bound by memory, for 16-bit logits nearly by
-// the exponentials (one an entry: 16 of an SM's 128 lanes).
+// Forward, the logits are read once.  Rows of up to eight entries take a
+// thread, rows of up to 1,024 a group of 2 to 32 lanes that holds them in
+// registers, 16 (32) entries a lane.  Longer rows take a block: every thread
+// keeps a running maximum with the sums below it, brought to a new maximum when
+// one comes, and the threads' sums are joined at the row's.  Bound by memory,
+// for 16-bit logits nearly by issue: six instructions an entry.
 //
-// The k largest: the k-th largest of the threads' maxima is no larger than the
-// k-th largest entry, so only threads whose maximum reaches it look at their
-// entries again, and only entries that reach it are listed: k and a few.  Their
-// order is counted out by (value, lowest index).  Should the list run over
-// (rows of equal values), the k largest are drawn one by one instead.
+// The k largest of a row in registers are drawn one by one: each lane knows its
+// largest, and only the lane that gave one up looks for the next.  In longer
+// rows the k-th largest of the threads' maxima is no larger than the k-th
+// largest entry, so only entries of threads whose maximum reaches it are looked
+// at again, by the whole warp, and only those that reach it are listed: k and a
+// few.  Their order is counted out by (value, lowest index).  Should the list
+// run over (rows of equal values), or hold NaN, the k largest are drawn one by
+// one instead.
 //
-// Rows of up to 32 entries take a thread, up to 1,024 a warp, else a block.
 // Addition has one order throughout: equal rows give equal bits.
 #include "policy.h"
 #include "values.cuh"
@@ -22,11 +26,12 @@
 namespace av {
 namespace {
 
-constexpr int kTiny = 32;          // entries of a row that a thread takes
+constexpr int kTiny = 8;           // entries of a row that a thread takes
 constexpr int kTinyThreads = 128;
-constexpr int kNarrow = 1024;      // entries of a row that a warp takes
+constexpr int kNarrow = 1024;      // entries of a row that a group of lanes takes
 constexpr int kNarrowThreads = 256;
 constexpr int kWideThreads = 512;
+constexpr int kGradThreads = 256;  // of a block that takes a part of a row's gradient
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -77,32 +82,41 @@ __device__ __forceinline__ uint64_t rank_key(float x, uint32_t j)
     return u ? (uint64_t)u << 32 | (uint32_t)~j : 0;
 }
 
+// And back.
+__device__ __forceinline__ float value_of(uint32_t u)
+{
+    return u == 0xffffffffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
 // The running maximum and the sums of exp(x - m) and exp(x - m) (x - m).
 struct Sums {
-    float m, e, ex;
-    uint32_t top;  // order_of the largest, NaN included
+    float m;
+    float2 e, ex;
 };
 
 __device__ __forceinline__ void raise(Sums &s, float m)
 {
-    const float d = s.m - m;  // (-inf where an infinite logit comes: the sums are NaN from there on, or 0)
-    float c = d;
-    const float k = exp_below(c);
-    s.ex = k * (s.ex + s.e * c);
-    s.e *= k;
+    float d = s.m - m;  // (-inf where an infinite logit comes: the sums are NaN from there on, or 0)
+    const float k = exp_below(d);
+    const float2 k2 = make_float2(k, k);
+    s.ex = mul2(k2, fma2(s.e, make_float2(d, d), s.ex));
+    s.e = mul2(s.e, k2);
     s.m = m;
 }
 
-__device__ __forceinline__ void add(Sums &s, float x)
+// Two entries, none above the maximum.
+__device__ __forceinline__ void add(Sums &s, float2 x)
 {
-    float d = x - s.m;
-    const float p = exp_below(d);
-    s.e += p;
-    s.ex = fmaf(p, d, s.ex);
+    float2 d = add2(x, make_float2(-s.m, -s.m));
+    d.x = max_nan(d.x, -200.0f);
+    d.y = max_nan(d.y, -200.0f);
+    const float2 t = mul2(d, make_float2(kLog2e, kLog2e)), p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+    s.e = add2(s.e, p);
+    s.ex = fma2(p, d, s.ex);
 }
 
 // kN entries at a time.
-template <bool kTop, int kN>
+template <int kN>
 __device__ __forceinline__ void take(Sums &s, const float (&x)[kN])
 {
     float m = x[0];
@@ -112,16 +126,8 @@ __device__ __forceinline__ void take(Sums &s, const float (&x)[kN])
     if (m > s.m)
         raise(s, m);
 #pragma unroll
-    for (int k = 0; k < kN; ++k)
-        add(s, x[k]);
-    if (kTop) {
-        bool bad = false;
-#pragma unroll
-        for (int k = 0; k < kN; ++k)
-            bad |= x[k] != x[k];
-        const uint32_t u = bad ? 0xffffffffu : order_of(m);
-        s.top = u > s.top ? u : s.top;
-    }
+    for (int k = 0; k < kN; k += 2)
+        add(s, make_float2(x[k], k + 1 < kN ? x[k + 1] : no_value()));
 }
 
 // A row of logits seen in packs of 16 bytes: entries before the first boundary,
@@ -158,52 +164,37 @@ struct Row {
     }
 };
 
-// All threads of the row: a warp, or the block.
-template <int kGroup>
-__device__ __forceinline__ void group_sync()
-{
-    if (kGroup == 32)
-        __syncwarp();
-    else
-        __syncthreads();
-}
-
-template <int kGroup, class F>
+template <class F>
 __device__ __forceinline__ float reduce(float v, float *slots, F f)
 {
 #pragma unroll
     for (int o = 16; o; o >>= 1)
         v = f(v, __shfl_xor_sync(~0u, v, o));
-    if (kGroup == 32)
-        return v;
     __syncthreads();
     if ((threadIdx.x & 31) == 0)
         slots[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = slots[threadIdx.x & (kGroup / 32 - 1)];
+    v = slots[threadIdx.x & (kWideThreads / 32 - 1)];
 #pragma unroll
-    for (int o = kGroup / 64; o; o >>= 1)
+    for (int o = kWideThreads / 64; o; o >>= 1)
         v = f(v, __shfl_xor_sync(~0u, v, o));
     return v;
 }
 
-constexpr int kListed = 512;  // candidates of a block's row, and of a warp's:
-constexpr int kListedWarp = 96;
+constexpr int kListed = 512;  // candidates of a row
 
-template <int kGroup>
 struct Scratch {
-    static constexpr int kWarps = kGroup / 32;
+    static constexpr int kWarps = kWideThreads / 32;
     float slots[kWarps];
     uint32_t heads[kWarps * AV_MAX_TOP];
     uint32_t floor;
     int count;
     uint64_t best[kWarps];
-    uint64_t list[kGroup == 32 ? kListedWarp : kListed];
+    uint64_t list[kListed];
 };
 
-// The k-th largest of the threads' values (0 where there are fewer).
-template <int kGroup>
-__device__ uint32_t kth(uint32_t v, int k, Scratch<kGroup> &s)
+// The k-th largest of the threads' values.
+__device__ uint32_t kth(uint32_t v, int k, Scratch &s)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t last = 0;
@@ -212,34 +203,35 @@ __device__ uint32_t kth(uint32_t v, int k, Scratch<kGroup> &s)
         const uint32_t holders = __ballot_sync(~0u, v == last);
         if (lane == __ffs(holders) - 1)
             v = 0;
-        if (kGroup > 32 && lane == 0)
+        if (lane == 0)
             s.heads[warp * AV_MAX_TOP + i] = last;
     }
-    if (kGroup == 32)
-        return last;
     __syncthreads();
     if (warp == 0) {  // each warp's are in order: a lane holds the next of one
         int at = 0;
         for (int i = 0; i < k; ++i) {
-            const uint32_t u = lane < kGroup / 32 && at < k ? s.heads[lane * AV_MAX_TOP + at] : 0;
+            const uint32_t u = lane < Scratch::kWarps && at < k ? s.heads[lane * AV_MAX_TOP + at] : 0;
             last = __reduce_max_sync(~0u, u);
-            const uint32_t holders = __ballot_sync(~0u, u == last && lane < kGroup / 32);
+            const uint32_t holders = __ballot_sync(~0u, u == last && lane < Scratch::kWarps);
             at += lane == __ffs(holders) - 1;
         }
-        if (lane == 0)
+        if (lane == 0) {
             s.floor = last;
+            s.count = 0;
+        }
     }
     __syncthreads();
     return s.floor;
 }
 
-// f(value, index) for this thread's entries of the row.
-template <int kGroup, bool kMask, class T, class F>
-__device__ __forceinline__ void entries(const Row<T> &row, int thread, F f)
+// f(value, index) for the entries of the row that `thread` takes, seen by
+// thread `lane` of `lanes`.
+template <bool kMask, class T, class F>
+__device__ __forceinline__ void entries(const Row<T> &row, int thread, int lane, int lanes, F f)
 {
-    for (int i = thread; i < row.loose(); i += kGroup)
+    for (int i = thread + lane * kWideThreads; i < row.loose(); i += lanes * kWideThreads)
         f(row.template entry<kMask>(row.loose_at(i)), row.loose_at(i));
-    for (int i = thread; i < row.packs; i += kGroup) {
+    for (int i = thread + lane * kWideThreads; i < row.packs; i += lanes * kWideThreads) {
         float v[Row<T>::kPack];
         row.template open<kMask>(row.raw(i), i, v);
 #pragma unroll
@@ -248,44 +240,44 @@ __device__ __forceinline__ void entries(const Row<T> &row, int thread, F f)
     }
 }
 
-template <class T, int kGroup, int kThreads, bool kMask, bool kTop>
-__global__ __launch_bounds__(kThreads) void logp_kernel(const LogpArgs a, int top, float *logp, float *entropy,
-                                                        float *peak, float *logz, float *top_logp, int32_t *top_index)
+template <class T, bool kMask, bool kTop>
+__global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs a, int top, float *logp, float *entropy,
+                                                                 float *peak, float *logz, float *top_logp,
+                                                                 int32_t *top_index)
 {
     constexpr int kPack = Row<T>::kPack, kAhead = 4;
-    __shared__ Scratch<kGroup> scratch[kThreads / kGroup];
-    Scratch<kGroup> &s = scratch[threadIdx.x / kGroup];
-    const int thread = threadIdx.x % kGroup;
-    const int64_t groups = (int64_t)gridDim.x * (kThreads / kGroup);
-    for (int64_t r = (int64_t)blockIdx.x * (kThreads / kGroup) + threadIdx.x / kGroup; r < a.rows; r += groups) {
+    __shared__ Scratch s;
+    const int thread = threadIdx.x;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row((const T *)a.logits + r * a.stride, kMask ? a.mask + r * a.mask_stride : nullptr, a.V);
-        Sums q{kLowest, 0.0f, 0.0f, 0u};
+        Sums q{kLowest, make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
         int i = thread;
-        for (; i + (kAhead - 1) * kGroup < row.packs; i += kAhead * kGroup) {
+        for (; i + (kAhead - 1) * kWideThreads < row.packs; i += kAhead * kWideThreads) {
             uint4 raw[kAhead];
 #pragma unroll
             for (int k = 0; k < kAhead; ++k)
-                raw[k] = row.raw(i + k * kGroup);
+                raw[k] = row.raw(i + k * kWideThreads);
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 float v[kPack];
-                row.template open<kMask>(raw[k], i + k * kGroup, v);
-                take<kTop>(q, v);
+                row.template open<kMask>(raw[k], i + k * kWideThreads, v);
+                take(q, v);
             }
         }
-        for (; i < row.packs; i += kGroup) {
+        for (; i < row.packs; i += kWideThreads) {
             float v[kPack];
             row.template open<kMask>(row.raw(i), i, v);
-            take<kTop>(q, v);
+            take(q, v);
         }
-        for (int j = thread; j < row.loose(); j += kGroup) {
+        for (int j = thread; j < row.loose(); j += kWideThreads) {
             const float v[1] = {row.template entry<kMask>(row.loose_at(j))};
-            take<kTop>(q, v);
+            take(q, v);
         }
-        const float m = reduce<kGroup>(q.m, s.slots, [](float x, float y) { return fmaxf(x, y); });
+        const float mine = q.m;
+        const float m = reduce(mine, s.slots, [](float x, float y) { return fmaxf(x, y); });
         raise(q, m);
         auto plus = [](float x, float y) { return x + y; };
-        const float e = reduce<kGroup>(q.e, s.slots, plus), ex = reduce<kGroup>(q.ex, s.slots, plus);
+        const float e = reduce(q.e.x + q.e.y, s.slots, plus), ex = reduce(q.ex.x + q.ex.y, s.slots, plus);
         const bool some = e != 0.0f;  // (NaN counts)
         const float z = some ? logf(e) : no_value();
         if (thread == 0) {
@@ -305,36 +297,35 @@ __global__ __launch_bounds__(kThreads) void logp_kernel(const LogpArgs a, int to
         }
         if (!kTop)
             continue;
-        const uint32_t floor = kth<kGroup>(q.top, top, s);
-        if (thread == 0)
-            s.count = 0;
-        group_sync<kGroup>();
-        constexpr int kRoom = kGroup == 32 ? kListedWarp : kListed;
-        if (q.top >= floor && q.top != 0) {
-            entries<kGroup, kMask>(row, thread, [&](float v, int j) {
+        // (a thread without an entry stands for the lowest value, below which no entry is)
+        const uint32_t highest = order_of(mine), floor = kth(highest, top, s);
+        uint32_t again = __ballot_sync(~0u, highest >= floor);
+        while (again) {  // the warp looks at one thread's entries after another
+            const int lane = __ffs(again) - 1;
+            again &= again - 1;
+            entries<kMask>(row, (thread & ~31) + lane, thread & 31, 32, [&](float v, int j) {
                 const uint32_t u = order_of(v);
                 if (u >= floor && u != 0) {
                     const int at = atomicAdd(&s.count, 1);
-                    if (at < kRoom)
+                    if (at < kListed)
                         s.list[at] = rank_key(v, j);
                 }
             });
         }
-        group_sync<kGroup>();
+        __syncthreads();
         const int count = s.count;
-        if (count <= kRoom) {
-            for (int c = thread; c < count; c += kGroup) {
-                const uint64_t mine = s.list[c];
+        if (count <= kListed && e == e) {
+            for (int c = thread; c < count; c += kWideThreads) {
+                const uint64_t key = s.list[c];
                 int rank = 0;
                 for (int o = 0; o < count; ++o)
-                    rank += s.list[o] > mine;
+                    rank += s.list[o] > key;
                 if (rank < top) {
-                    const int j = (int)~(uint32_t)mine;
-                    top_index[r * top + rank] = j;
-                    top_logp[r * top + rank] = (to_f32(row.x[j]) - m) - z;
+                    top_index[r * top + rank] = (int)~(uint32_t)key;
+                    top_logp[r * top + rank] = (value_of((uint32_t)(key >> 32)) - m) - z;
                 }
             }
-            for (int k = count + thread; k < top; k += kGroup) {  // fewer than asked for
+            for (int k = count + thread; k < top; k += kWideThreads) {  // fewer than asked for
                 top_index[r * top + k] = -1;
                 top_logp[r * top + k] = no_value();
             }
@@ -342,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void logp_kernel(const LogpArgs a, int to
             uint64_t last = ~0ull;
             for (int k = 0; k < top; ++k) {
                 uint64_t best = 0;
-                entries<kGroup, kMask>(row, thread, [&](float v, int j) {
+                entries<kMask>(row, thread, 0, 1, [&](float v, int j) {
                     const uint64_t key = rank_key(v, j);
                     best = key < last && key > best ? key : best;
                 });
@@ -351,23 +342,124 @@ __global__ __launch_bounds__(kThreads) void logp_kernel(const LogpArgs a, int to
                     const uint64_t u = __shfl_xor_sync(~0u, best, o);
                     best = u > best ? u : best;
                 }
-                if (kGroup > 32) {
-                    __syncthreads();
-                    if ((threadIdx.x & 31) == 0)
-                        s.best[threadIdx.x >> 5] = best;
-                    __syncthreads();
-                    for (int w = 0; w < kGroup / 32; ++w)
-                        best = s.best[w] > best ? s.best[w] : best;
-                }
+                __syncthreads();
+                if ((thread & 31) == 0)
+                    s.best[thread >> 5] = best;
+                __syncthreads();
+                for (int w = 0; w < Scratch::kWarps; ++w)
+                    best = s.best[w] > best ? s.best[w] : best;
                 last = best;
                 if (thread == 0) {
-                    const int j = (int)~(uint32_t)best;
-                    top_index[r * top + k] = best ? j : -1;
-                    top_logp[r * top + k] = best ? (to_f32(row.x[j]) - m) - z : no_value();
+                    top_index[r * top + k] = best ? (int)~(uint32_t)best : -1;
+                    top_logp[r * top + k] = best ? (value_of((uint32_t)(best >> 32)) - m) - z : no_value();
                 }
             }
         }
-        group_sync<kGroup>();  // (the list is the next row's)
+        __syncthreads();  // (the list is the next row's)
+    }
+}
+
+// A lane's entries of a row: kPer of them, kVec neighbours from each load.
+template <class T, int kVec, int kLanes, int kPer>
+struct Held {
+    // the place of entry k
+    __device__ static __forceinline__ int at(int k, int lane) { return (k / kVec * kLanes + lane) * kVec + k % kVec; }
+    __device__ static __forceinline__ void load(float (&v)[kPer], const T *row, const uint8_t *mask, int V, int lane)
+    {
+#pragma unroll
+        for (int c = 0; c < kPer; c += kVec) {
+            const int j = at(c, lane);
+            T q[kVec];
+            if (j < V) {
+                if constexpr (kVec == 1)
+                    q[0] = row[j];
+                else
+                    *reinterpret_cast<uint4 *>(q) = *reinterpret_cast<const uint4 *>(row + j);
+            }
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                v[c + e] = j < V && !(mask && mask[j + e] == 0) ? to_f32(q[e]) : no_value();
+        }
+    }
+};
+
+// kLanes lanes a row of at most kLanes kPer entries, all in registers.
+template <class T, int kVec, int kLanes, int kPer>
+__global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpArgs a, int top, float *logp,
+                                                                     float *entropy, float *peak, float *logz,
+                                                                     float *top_logp, int32_t *top_index)
+{
+    using H = Held<T, kVec, kLanes, kPer>;
+    const int lane = threadIdx.x % kLanes;
+    const int64_t r = ((int64_t)blockIdx.x * kNarrowThreads + threadIdx.x) / kLanes;
+    const bool here = r < a.rows;  // (lanes without a row go along: shuffles are the warp's)
+    const T *x = (const T *)a.logits + (here ? r : 0) * a.stride;
+    const uint8_t *mask = a.mask ? a.mask + (here ? r : 0) * a.mask_stride : nullptr;
+    const int64_t tok = here ? token_of(a.tokens, a.token_bytes, r) : -1;
+    const bool given = tok >= 0 && tok < a.V;
+    float v[kPer], m = kLowest;
+    H::load(v, x, mask, a.V, lane);
+    const float wanted = given && !(mask && mask[tok] == 0) ? to_f32(x[tok]) : no_value();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+        m = fmaxf(m, v[k]);
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1)
+        m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    Sums q{m, make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+    for (int k = 0; k < kPer; k += 2)
+        add(q, make_float2(v[k], v[k + 1]));
+    float e = q.e.x + q.e.y, ex = q.ex.x + q.ex.y;
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) {
+        e += __shfl_xor_sync(~0u, e, o);
+        ex += __shfl_xor_sync(~0u, ex, o);
+    }
+    const bool some = e != 0.0f;
+    const float z = some ? logf(e) : no_value();
+    if (here && lane == 0) {
+        logp[r] = given ? (some ? (wanted - m) - z : no_value()) : 0.0f;
+        if (entropy)
+            entropy[r] = some ? z - ex / e : 0.0f;
+        if (peak)
+            peak[r] = some ? m : no_value();
+        if (logz)
+            logz[r] = z;
+    }
+    if (top == 0)
+        return;
+    uint32_t u[kPer], best = 0;
+    int at = 0;  // of this lane's largest
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        u[k] = order_of(v[k]);
+        at = u[k] > best ? k : at;
+        best = u[k] > best ? u[k] : best;
+    }
+    for (int i = 0; i < top; ++i) {
+        const uint64_t mine = best ? (uint64_t)best << 32 | (uint32_t)~H::at(at, lane) : 0;
+        uint64_t key = mine;
+#pragma unroll
+        for (int o = kLanes / 2; o; o >>= 1) {
+            const uint64_t other = __shfl_xor_sync(~0u, key, o);
+            key = other > key ? other : key;
+        }
+        if (here && lane == 0) {
+            top_index[r * top + i] = key ? (int)~(uint32_t)key : -1;
+            top_logp[r * top + i] = key ? (value_of((uint32_t)(key >> 32)) - m) - z : no_value();
+        }
+        if (key == mine && key) {  // this lane's: the next of it
+            const int gone = at;
+            best = 0;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                u[k] = k == gone ? 0 : u[k];
+                at = u[k] > best ? k : at;
+                best = u[k] > best ? u[k] : best;
+            }
+        }
+        __syncwarp();
     }
 }
 
@@ -388,20 +480,21 @@ __global__ __launch_bounds__(kTinyThreads) void logp_tiny_kernel(const LogpArgs 
         v[j] = j < a.V && (!kMask || mask[j] != 0) ? to_f32(x[j]) : no_value();
         m = fmaxf(m, v[j]);
     }
-    Sums q{m, 0.0f, 0.0f, 0u};
+    Sums q{m, make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
     const int64_t tok = token_of(a.tokens, a.token_bytes, r);
     float given = no_value();
 #pragma unroll
-    for (int j = 0; j < kMost; ++j) {
-        if (j < a.V)
-            add(q, v[j]);
+    for (int j = 0; j < kMost; ++j)
         given = j == tok ? v[j] : given;
-    }
-    const bool some = q.e != 0.0f;
-    const float z = some ? logf(q.e) : no_value();
+#pragma unroll
+    for (int j = 0; j < kMost; j += 2)
+        add(q, make_float2(v[j], v[j + 1]));
+    const float e = q.e.x + q.e.y, ex = q.ex.x + q.ex.y;
+    const bool some = e != 0.0f;
+    const float z = some ? logf(e) : no_value();
     logp[r] = tok >= 0 && tok < a.V ? (some ? (given - m) - z : no_value()) : 0.0f;
     if (entropy)
-        entropy[r] = some ? z - q.ex / q.e : 0.0f;
+        entropy[r] = some ? z - ex / e : 0.0f;
     if (peak)
         peak[r] = some ? m : no_value();
     if (logz)
@@ -457,34 +550,69 @@ __device__ __forceinline__ float slope_at(const Slope &s, float x)
     return -p * fmaf(s.de, lp, s.c);
 }
 
-// A block (or a warp) takes a row, or with gridDim.y a part of it.
-template <class T, int kGroup, int kThreads, bool kMask>
-__global__ __launch_bounds__(kThreads) void logp_grad_kernel(const LogpArgs a, const float *dlogp,
-                                                             const float *dentropy, const float *peak,
-                                                             const float *logz, const float *entropy, T *dlogits,
-                                                             int64_t dstride, bool packed)
+// An entry's gradient whole.
+template <bool kMask>
+__device__ __forceinline__ float gradient_at(const Slope &s, float x, int j)
 {
-    constexpr int kPack = Row<T>::kPack, kAhead = 4;
-    const int64_t r = (int64_t)blockIdx.x * (kThreads / kGroup) + threadIdx.x / kGroup;
+    if (!s.some || (kMask && x == no_value()))
+        return 0.0f;
+    return slope_at(s, x) + (j == s.tok && x != no_value() ? s.dl : 0.0f);
+}
+
+// kLanes lanes a row of at most kLanes kPer entries.
+template <class T, int kVec, int kLanes, int kPer>
+__global__ __launch_bounds__(kNarrowThreads) void logp_narrow_grad_kernel(const LogpArgs a, const float *dlogp,
+                                                                          const float *dentropy, const float *peak,
+                                                                          const float *logz, const float *entropy,
+                                                                          T *dlogits, int64_t dstride)
+{
+    using H = Held<T, kVec, kLanes, kPer>;
+    const int lane = threadIdx.x % kLanes;
+    const int64_t r = ((int64_t)blockIdx.x * kNarrowThreads + threadIdx.x) / kLanes;
     if (r >= a.rows)
         return;
+    float v[kPer];
+    H::load(v, (const T *)a.logits + r * a.stride, a.mask ? a.mask + r * a.mask_stride : nullptr, a.V, lane);
+    const Slope s = slope_of(a, r, dlogp, dentropy, peak, logz, entropy);
+    T *dx = dlogits + r * dstride;
+#pragma unroll
+    for (int c = 0; c < kPer; c += kVec) {
+        const int j = H::at(c, lane);
+        if (j >= a.V)
+            continue;
+        T o[kVec];
+        // (an absent entry's logit is -inf and its gradient 0 with or without a mask)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+            o[e] = from_f32<T>(gradient_at<true>(s, v[c + e], j + e));
+        if constexpr (kVec == 1)
+            dx[j] = o[0];
+        else
+            *reinterpret_cast<uint4 *>(dx + j) = *reinterpret_cast<const uint4 *>(o);
+    }
+}
+
+// A block takes a part of a row.
+template <class T, bool kMask>
+__global__ __launch_bounds__(kGradThreads) void logp_wide_grad_kernel(const LogpArgs a, const float *dlogp,
+                                                                      const float *dentropy, const float *peak,
+                                                                      const float *logz, const float *entropy,
+                                                                      T *dlogits, int64_t dstride, bool packed)
+{
+    constexpr int kPack = Row<T>::kPack, kAhead = 4;
+    const int64_t r = blockIdx.x;
     const Row<T> row((const T *)a.logits + r * a.stride, kMask ? a.mask + r * a.mask_stride : nullptr, a.V);
     const Slope s = slope_of(a, r, dlogp, dentropy, peak, logz, entropy);
     T *dx = dlogits + r * dstride;
-    const int thread = threadIdx.x % kGroup + blockIdx.y * kGroup, step = kGroup * gridDim.y;
-    auto value = [&](float x, int j) {
-        if (!s.some || (kMask && x == no_value()))
-            return 0.0f;
-        return slope_at(s, x) + (j == s.tok && x != no_value() ? s.dl : 0.0f);
-    };
+    const int thread = threadIdx.x + blockIdx.y * kGradThreads, step = kGradThreads * gridDim.y;
     if (!packed) {  // dlogits' rows begin elsewhere in 16 bytes than those of logits
         for (int j = thread; j < a.V; j += step)
-            dx[j] = from_f32<T>(value(row.template entry<kMask>(j), j));
+            dx[j] = from_f32<T>(gradient_at<kMask>(s, row.template entry<kMask>(j), j));
         return;
     }
     for (int i = thread; i < row.loose(); i += step) {
         const int j = row.loose_at(i);
-        dx[j] = from_f32<T>(value(row.template entry<kMask>(j), j));
+        dx[j] = from_f32<T>(gradient_at<kMask>(s, row.template entry<kMask>(j), j));
     }
     for (int i0 = thread; i0 < row.packs; i0 += kAhead * step) {
         uint4 raw[kAhead];
@@ -508,7 +636,7 @@ __global__ __launch_bounds__(kThreads) void logp_grad_kernel(const LogpArgs a, c
             } else {
 #pragma unroll
                 for (int e = 0; e < kPack; ++e)
-                    o[e] = from_f32<T>(value(v[e], j + e));
+                    o[e] = from_f32<T>(gradient_at<kMask>(s, v[e], j + e));
             }
             *reinterpret_cast<uint4 *>(dx + j) = out;
         }
@@ -529,10 +657,7 @@ __global__ __launch_bounds__(kTinyThreads) void logp_grad_tiny_kernel(const Logp
 #pragma unroll 8
     for (int j = 0; j < a.V; ++j) {
         const float v = kMask && a.mask[r * a.mask_stride + j] == 0 ? no_value() : to_f32(x[j]);
-        const float g = !s.some || (kMask && v == no_value())
-                            ? 0.0f
-                            : slope_at(s, v) + (j == s.tok && v != no_value() ? s.dl : 0.0f);
-        dlogits[r * dstride + j] = from_f32<T>(g);
+        dlogits[r * dstride + j] = from_f32<T>(gradient_at<kMask>(s, v, j));
     }
 }
 
@@ -549,6 +674,32 @@ void with_flag(bool v, F f)
         f(std::false_type());
 }
 
+// Calls f with the lanes and the entries a lane for rows of V entries.
+template <class F>
+void with_lanes(int V, F f)
+{
+    using std::integral_constant;
+    const integral_constant<int, 16> sixteen;
+    if (V <= 32)
+        f(integral_constant<int, 2>(), sixteen);
+    else if (V <= 64)
+        f(integral_constant<int, 4>(), sixteen);
+    else if (V <= 128)
+        f(integral_constant<int, 8>(), sixteen);
+    else if (V <= 256)
+        f(integral_constant<int, 16>(), sixteen);
+    else if (V <= 512)
+        f(integral_constant<int, 32>(), sixteen);
+    else
+        f(integral_constant<int, 32>(), integral_constant<int, 32>());
+}
+
+// Rows of whole 16-byte packs.
+bool packs(const void *p, int64_t rows, int V, int64_t stride, int64_t e)
+{
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && V * e % 16 == 0 && (rows <= 1 || stride * e % 16 == 0);
+}
+
 }  // namespace
 
 cudaError_t launch_logp(const LogpArgs &a, int top, float *logp, float *entropy, float *peak, float *logz,
@@ -556,30 +707,30 @@ cudaError_t launch_logp(const LogpArgs &a, int top, float *logp, float *entropy,
 {
     with_type(a.dtype, [&](auto v) {
         using T = decltype(v);
+        if (a.V > kTiny && a.V <= kNarrow) {
+            with_lanes(a.V, [&](auto lanes, auto per) {
+                auto run = [&](auto kernel) {
+                    kernel<<<(unsigned)up(a.rows * lanes.value, kNarrowThreads), kNarrowThreads, 0, st>>>(
+                        a, top, logp, entropy, peak, logz, top_logp, top_index);
+                };
+                if (packs(a.logits, a.rows, a.V, a.stride, sizeof(T)))
+                    run(logp_narrow_kernel<T, 16 / sizeof(T), lanes.value, per.value>);
+                else
+                    run(logp_narrow_kernel<T, 1, lanes.value, per.value>);
+            });
+            return;
+        }
         with_flag(a.mask != nullptr, [&](auto mask) {
             if (a.V <= kTiny) {
-                auto run = [&](auto kernel) {
-                    kernel<<<(unsigned)up(a.rows, kTinyThreads), kTinyThreads, 0, st>>>(a, top, logp, entropy, peak,
-                                                                                        logz, top_logp, top_index);
-                };
-                if (a.V <= 8)
-                    run(logp_tiny_kernel<T, 8, mask.value>);
-                else
-                    run(logp_tiny_kernel<T, kTiny, mask.value>);
+                logp_tiny_kernel<T, kTiny, mask.value><<<(unsigned)up(a.rows, kTinyThreads), kTinyThreads, 0, st>>>(
+                    a, top, logp, entropy, peak, logz, top_logp, top_index);
                 return;
             }
             with_flag(top > 0, [&](auto tops) {
-                if (a.V <= kNarrow) {
-                    const int64_t blocks = up(a.rows, kNarrowThreads / 32), most = 152 * 8 * 4;
-                    logp_kernel<T, 32, kNarrowThreads, mask.value, tops.value>
-                        <<<(unsigned)(blocks < most ? blocks : most), kNarrowThreads, 0, st>>>(
-                            a, top, logp, entropy, peak, logz, top_logp, top_index);
-                } else {
-                    const int64_t most = 152 * 4 * 4;
-                    logp_kernel<T, kWideThreads, kWideThreads, mask.value, tops.value>
-                        <<<(unsigned)(a.rows < most ? a.rows : most), kWideThreads, 0, st>>>(
-                            a, top, logp, entropy, peak, logz, top_logp, top_index);
-                }
+                const int64_t most = 152 * 4 * 4;
+                logp_wide_kernel<T, mask.value, tops.value>
+                    <<<(unsigned)(a.rows < most ? a.rows : most), kWideThreads, 0, st>>>(a, top, logp, entropy, peak,
+                                                                                      logz, top_logp, top_index);
             });
         });
     });
@@ -594,20 +745,30 @@ cudaError_t launch_logp_grad(const LogpArgs &a, const float *dlogp, const float 
         using T = decltype(v);
         T *dx = (T *)dlogits;
         const int64_t e = sizeof(T);
+        if (a.V > kTiny && a.V <= kNarrow) {
+            with_lanes(a.V, [&](auto lanes, auto per) {
+                auto run = [&](auto kernel) {
+                    kernel<<<(unsigned)up(a.rows * lanes.value, kNarrowThreads), kNarrowThreads, 0, st>>>(
+                        a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride);
+                };
+                if (packs(a.logits, a.rows, a.V, a.stride, e) && packs(dlogits, a.rows, a.V, dlogit_stride, e))
+                    run(logp_narrow_grad_kernel<T, 16 / sizeof(T), lanes.value, per.value>);
+                else
+                    run(logp_narrow_grad_kernel<T, 1, lanes.value, per.value>);
+            });
+            return;
+        }
+        // whether dlogits' rows begin where in 16 bytes those of logits do
         const bool packed = ((reinterpret_cast<uintptr_t>(dlogits) ^ reinterpret_cast<uintptr_t>(a.logits)) & 15) == 0 &&
                             (a.rows <= 1 || (dlogit_stride - a.stride) * e % 16 == 0);
         with_flag(a.mask != nullptr, [&](auto mask) {
             if (a.V <= kTiny) {
                 logp_grad_tiny_kernel<T, mask.value><<<(unsigned)up(a.rows, kTinyThreads), kTinyThreads, 0, st>>>(
                     a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride);
-            } else if (a.V <= kNarrow) {
-                logp_grad_kernel<T, 32, kNarrowThreads, mask.value>
-                    <<<(unsigned)up(a.rows, kNarrowThreads / 32), kNarrowThreads, 0, st>>>(
-                        a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride, packed);
             } else {
                 const int parts = (int)up(a.V, 16384);  // (of a row; blocks of some 16,384 entries)
-                logp_grad_kernel<T, kNarrowThreads, kNarrowThreads, mask.value>
-                    <<<dim3((unsigned)a.rows, (unsigned)(parts < 65535 ? parts : 65535)), kNarrowThreads, 0, st>>>(
+                logp_wide_grad_kernel<T, mask.value>
+                    <<<dim3((unsigned)a.rows, (unsigned)(parts < 65535 ? parts : 65535)), kGradThreads, 0, st>>>(
                         a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride, packed);
             }
         });
