@@ -16,7 +16,8 @@ SOURCES = [os.path.join(CSRC, f) for f in ("autoverse.cu", "k_fast_u8.cu", "k_fa
                                             "k_scan.cu", "k_logp.cu", "k_ffn.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "launch.h", "k_fast_impl.cuh", "k_warp_impl.cuh",
                                                      "k_memo_impl.cuh", "block_step.cuh", "small_step.cuh",
-                                                     "variant_keys.cuh", "policy.h", "values.cuh")] + [
+                                                     "variant_keys.cuh", "policy.h", "values.cuh",
+                                                     "async.cuh", "tensor_map.h")] + [
     os.path.join(ROOT, "include", "autoverse.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -15,10 +15,9 @@
 //
 // Warps: one issues copies (TMA), one products, four take accumulators to
 // memory while the next tile's products run (two sets of 256 TMEM columns).
-#include <cuda.h>
-
 #include "async.cuh"
 #include "policy.h"
+#include "tensor_map.h"
 #include "values.cuh"
 
 namespace av {
@@ -535,45 +534,6 @@ __global__ void ffn_parts_kernel(int64_t rows, int64_t cols, int splits, const f
 
 // ------------------------------------------------------------ host
 
-using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                            const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                            CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-Encode encoder()
-{
-    static const Encode fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) !=
-                cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            return (Encode) nullptr;
-        return (Encode)p;
-    }();
-    return fn;
-}
-
-// dims, box: innermost first; strides of the outer dims in elements.
-bool make_map(CUtensorMap *map, int dtype, const void *p, int rank, const int64_t *dims, const int64_t *strides,
-              const int *box)
-{
-    const int64_t e = dtype == AV_F32 ? 4 : 2;
-    cuuint64_t d[3], s[2];
-    cuuint32_t b[3], one[3] = {1, 1, 1};
-    for (int i = 0; i < rank; ++i) {
-        d[i] = (cuuint64_t)dims[i];
-        b[i] = (cuuint32_t)box[i];
-        if (i > 0)
-            s[i - 1] = (cuuint64_t)(strides[i - 1] * e);
-    }
-    const CUtensorMapDataType type = dtype == AV_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                     : dtype == AV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                        : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    return encoder()(map, type, (cuuint32_t)rank, const_cast<void *>(p), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // An operand: [rows][cols], boxes of box_rows x 64 columns.
 bool operand_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64_t cols, int64_t stride, int box_rows)
 {
@@ -715,7 +675,7 @@ int64_t ffn_work_bytes(int64_t rows, int64_t D, int64_t H)
 cudaError_t launch_ffn(int64_t rows, int64_t D, int64_t H, int dtype, int act, const void *x, int64_t x_stride,
                        const void *w, void *h, int64_t h_stride, cudaStream_t st)
 {
-    if (!encoder())
+    if (!map_encoder())
         return cudaErrorNotSupported;
     auto run = [&](auto v) {
         using T = decltype(v);
@@ -731,7 +691,7 @@ cudaError_t launch_ffn_grad(int64_t rows, int64_t D, int64_t H, int dtype, int a
                             const void *x, int64_t x_stride, const void *w, void *dx, int64_t dx_stride, void *dw,
                             void *work, cudaStream_t st)
 {
-    if (!encoder())
+    if (!map_encoder())
         return cudaErrorNotSupported;
     float *parts = reinterpret_cast<float *>((char *)work + dgu_bytes(rows, H));
     auto run = [&](auto v) {

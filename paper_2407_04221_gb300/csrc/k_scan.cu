@@ -4,33 +4,34 @@
 //
 // Steps are affine maps h -> A h + H, and maps compose: a run of steps is one
 // map whatever its length.  A block takes 64 channels and chunks of 128 steps
-// (64 of 32-bit values, 32 or 64 of shorter sequences).  A warp takes eight of the channels: its
-// lanes are four pairs of them by eight runs of 16 steps, so that runs are
-// joined by shuffles and no warp waits for another.  Chunks come to shared
-// memory by asynchronous copies, the next ones under way during this one, and
-// results leave from the places of the inputs they came from; eight channels
-// of a step are 16 bytes, whose place in the row turns with the run, so that
-// lanes of different runs read different banks.  Both directions read and
-// write their arrays once: 3 and 5 values a step and channel.  The backward
-// pass makes the states again from the one kept at each chunk's start (4 bytes
-// a chunk and channel), so it neither reads h nor suffers its rounding.  Bound
-// by memory, and for 16-bit values nearly by issue: some 20 instructions a
-// value forward.
+// (64 of 32-bit values, 32 or 64 of shorter sequences).  A warp takes eight of
+// the channels: its lanes are four pairs of them by eight runs of 16 steps, so
+// that runs are joined by shuffles and no warp waits for another.  Chunks come
+// and go by TMA through shared memory, the next one under way during this one,
+// results leaving from the places of the inputs they came from.  The tensor
+// maps lay step k of all eight runs side by side, so that the 128-byte swizzle
+// sends lanes of different runs to different banks.  (Chunks that reach past
+// the sequence, and arrays that TMA does not take, go by cp.async or by single
+// values, to the same places.)  Both directions read and write their arrays
+// once: 3 and 5 values a step and channel.  The backward pass makes the states
+// again from the one kept at each chunk's start (4 bytes a chunk and channel),
+// so it neither reads h nor suffers its rounding.  Bound by memory, and for
+// 16-bit values by issue.
 //
-// Where channels alone fill the GPU, a block walks its channels' chunks in
-// order.  Where they do not, blocks take chunks as they come: a warp publishes
-// its chunk's map and takes its state from the maps of the chunks before it in
-// its group of 32 and the state at the group's start, in that fixed order,
-// whoever is ready first.  Places are drawn from a counter, so what a chunk
-// waits for was drawn before it.
+// A block walks its channels' chunks in order.  Where the channels would not
+// fill the GPU, a sequence is cut into segments: a first pass makes every
+// segment's map, a second walks the segments from the states that the maps
+// before them give, in one order.  The inputs are read twice then, but no block
+// waits for another.  Up to 16 steps of many channels take a thread each for
+// two channels.
 //
 // A step that begins an episode forgets the state even where it is NaN: in a
 // map this is a factor with its sign bit set, which survives composition.
-#include <stdlib.h>
-
 #include <type_traits>
 
+#include "async.cuh"
 #include "policy.h"
+#include "tensor_map.h"
 #include "values.cuh"
 
 namespace av {
@@ -40,8 +41,9 @@ constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kRuns = 8;         // runs of a chunk, a quarter of a warp's lanes each
 constexpr int kLongRun = 16;     // steps of a run at most
 constexpr int kSlab = 64;        // channels of a block, eight a warp, two a lane
-constexpr int kGroup = 32;       // chunks that share a start
 constexpr int kSms = 152;
+constexpr int kMaps = 32;        // maps of a block: a pair of channels each
+constexpr int64_t kBriefChannels = 4096;  // from where on brief sequences take a thread for two channels
 
 __device__ __forceinline__ float exp2_fast(float v)
 {
@@ -141,56 +143,23 @@ struct Args {
     float *last;                // h_last forward, dh0 backward: the state that leaves, or NULL
     float *states;              // [chunk][B D]: written forward (or NULL), read backward
     uint32_t slabs, chunks;     // blocks of channels, chunks of steps
+    uint32_t segments, per;     // segments of a sequence, chunks of a segment
+    Map2 *maps;                 // [slab][segment][kMaps], where there are several segments
     bool flat;                  // sequences lie side by side: channels are numbered through
     int in_bytes, out_bytes;    // of a copy: 16, 4, or 0 where values are copied one by one
-    int *ticket;                // NULL: a block walks all chunks
-    int *ready, *group_ready;   // [slab][warp][chunk], [slab][warp][group]
-    Map2 *maps;                 // [slab][warp][chunk][4]
-    float2 *group_state;        // [slab][warp][group][4]
-    int64_t limit_ns;
 };
-
-__device__ __forceinline__ int load_flag(const int *p)
-{
-    int v;
-    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ void store_flag(int *p)
-{
-    asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(1) : "memory");
-}
-__device__ __forceinline__ int64_t now_ns()
-{
-    int64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-
-// Waits for a flag; false when the limit passes first (a negative one: at once).
-__device__ __noinline__ bool wait_flag(const int *p, int64_t limit_ns)
-{
-    if (limit_ns < 0)
-        return false;
-    int64_t began = 0;
-    for (int spins = 0; load_flag(p) == 0; ++spins) {
-        if ((spins & 255) == 255) {
-            const int64_t t = now_ns();
-            if (!began)
-                began = t;
-            else if (t - began > limit_ns)
-                return false;
-        }
-    }
-    return true;
-}
+// The arrays for TMA: inputs, outputs.
+struct TensorMaps {
+    CUtensorMap in[3], out[2];
+};
 
 // What a block does next: chunk `place` chunks after its chain's first
 // (backward: from the end) of a slab of channels.
 struct Item {
     int64_t b, d, c;       // sequence and channel of the slab's first; that of the states
     int64_t b0;            // the sequence of its resets, -1 where it has several
-    uint32_t slab, place;
+    uint32_t slab, segment, place;
+    bool enters;           // the segment's first chunk
     int width;             // channels, or 0: there is nothing left to do
 };
 
@@ -200,21 +169,25 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
 }
 
 // Divisions are dear: one thread works an item out for the block.
-__device__ __forceinline__ void set_item(const Args &a, Item &t, uint32_t slab, uint32_t place, bool any)
+__device__ __forceinline__ void set_item(const Args &a, Item &t, uint32_t unit, uint32_t place)
 {
-    if (!any) {
+    t.slab = unit / a.segments;
+    if (t.slab >= a.slabs) {
         t.width = 0;
         return;
     }
+    t.segment = unit - t.slab * a.segments;
+    t.place = place;
+    t.enters = place == t.segment * a.per;
     int64_t left;
     if (a.flat) {
         t.b = 0;
-        t.d = (int64_t)slab * kSlab;
+        t.d = (int64_t)t.slab * kSlab;
         left = a.B * a.D - t.d;
     } else {
-        const uint32_t per = (uint32_t)((a.D + kSlab - 1) / kSlab);
-        t.b = slab / per;
-        t.d = (int64_t)(slab % per) * kSlab;
+        const uint32_t across = (uint32_t)((a.D + kSlab - 1) / kSlab);
+        t.b = t.slab / across;
+        t.d = (int64_t)(t.slab % across) * kSlab;
         left = a.D - t.d;
     }
     t.c = t.b * a.D + t.d;
@@ -225,88 +198,108 @@ __device__ __forceinline__ void set_item(const Args &a, Item &t, uint32_t slab, 
         if (t.c + t.width > (t.b0 + 1) * a.D)
             t.b0 = -1;
     }
-    t.slab = slab;
-    t.place = place;
 }
 
-// A chunk in shared memory is [step][64], eight channels' place in a row
-// turned by the step's run.
-template <int kRun>
+// The order of a block's items: units (a segment of a slab) gridDim.x apart,
+// the chunks of each in order.
+struct Order {
+    uint32_t unit, place, end;
+    __device__ __forceinline__ void open(const Args &a)
+    {
+        const uint32_t segment = unit % a.segments;
+        place = segment * a.per;
+        end = place + a.per < a.chunks ? place + a.per : a.chunks;
+    }
+    __device__ __forceinline__ void next(const Args &a, Item &t)
+    {
+        set_item(a, t, unit, place);
+        if (++place >= end) {
+            unit += gridDim.x;
+            open(a);
+        }
+    }
+};
+
+// A chunk of an array in shared memory: rows of 128 bytes, step k of run r in
+// row 8 k + r, its 16-byte pieces turned by r (the 128-byte swizzle).  32-bit
+// values are two such blocks of 32 channels.
+template <class T, int kRun>
 __device__ __forceinline__ int place_of(int step, int channel)
 {
-    return step * kSlab + ((channel >> 3 ^ (step / kRun & 7)) << 3 | (channel & 7));
+    const int r = step / kRun, row = step % kRun * kRuns + r;
+    if constexpr (sizeof(T) == 4)
+        return (channel >> 5) * (kRun * kRuns * 32) + row * 32 + (((channel & 31) >> 2 ^ r) << 2 | (channel & 3));
+    return row * 64 + ((channel >> 3 ^ r) << 3 | (channel & 7));
 }
+// Values between a run's steps.
+template <class T>
+__device__ constexpr int step_of() { return kRuns * 128 / (int)sizeof(T); }
 
 // Calls f(pointer, place) for all of a chunk's pieces of kPer channels that are
 // there, dealt to the block's threads; p: the array's first value of the chunk.
-template <int kRun, int kPer, class P, class F>
+template <class T, int kRun, int kPer, class P, class F>
 __device__ __forceinline__ void pieces(P *p, int64_t stride, int steps, int width, F f)
 {
-    constexpr int kAcross = kSlab / kPer, kDown = kThreads / kAcross, kSteps = kRun * kRuns;
+    constexpr int kAcross = kSlab / kPer, kDown = kThreads / kAcross;
     const int channel = threadIdx.x % kAcross * kPer, first = threadIdx.x / kAcross;
     if (channel >= width)
         return;
     p += first * stride + channel;
-    if (steps == kSteps) {
-#pragma unroll(kSteps / kDown < 8 ? kSteps / kDown : 8)
-        for (int k = first; k < kSteps; k += kDown, p += kDown * stride)
-            f(p, place_of<kRun>(k, channel));
-    } else {
-        for (int k = first; k < steps; k += kDown, p += kDown * stride)
-            f(p, place_of<kRun>(k, channel));
-    }
+#pragma unroll 4
+    for (int k = first; k < steps; k += kDown, p += kDown * stride)
+        f(p, place_of<T, kRun>(k, channel));
 }
 
 // A chunk of an array to shared memory, as far as there are steps and channels.
 template <class T, int kRun>
-__device__ __forceinline__ void bring(T *to, const void *from, int64_t st, int64_t sb, const Item &s, int64_t t0,
-                                      int steps, int bytes)
+__device__ __noinline__ void bring(T *to, const void *from, int64_t st, int64_t sb, const Item &s, int64_t t0,
+                                   int steps, int bytes)
 {
     const T *p = (const T *)from + t0 * st + s.b * sb + s.d;
-    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+    const uint32_t dst = smem_addr(to);
     if (bytes == 16)
-        pieces<kRun, 16 / sizeof(T)>(p, st, steps, s.width, [&](const T *q, int at) {
+        pieces<T, kRun, 16 / sizeof(T)>(p, st, steps, s.width, [&](const T *q, int at) {
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(at * sizeof(T))), "l"(q)
                          : "memory");
         });
     else if (bytes == 4)
-        pieces<kRun, 4 / sizeof(T)>(p, st, steps, s.width, [&](const T *q, int at) {
+        pieces<T, kRun, 4 / sizeof(T)>(p, st, steps, s.width, [&](const T *q, int at) {
             asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (uint32_t)(at * sizeof(T))), "l"(q)
                          : "memory");
         });
     else
-        pieces<kRun, 1>(p, st, steps, s.width, [&](const T *q, int at) { to[at] = *q; });
+        pieces<T, kRun, 1>(p, st, steps, s.width, [&](const T *q, int at) { to[at] = *q; });
 }
 
 // And back.
 template <class T, int kRun>
-__device__ __forceinline__ void take_out(const T *from, void *to, int64_t st, int64_t sb, const Item &s, int64_t t0,
-                                         int steps, int bytes)
+__device__ __noinline__ void take_out(const T *from, void *to, int64_t st, int64_t sb, const Item &s, int64_t t0,
+                                      int steps, int bytes)
 {
     T *p = (T *)to + t0 * st + s.b * sb + s.d;
     if (bytes == 16)
-        pieces<kRun, 16 / sizeof(T)>(p, st, steps, s.width, [&](T *q, int at) {
+        pieces<T, kRun, 16 / sizeof(T)>(p, st, steps, s.width, [&](T *q, int at) {
             *reinterpret_cast<uint4 *>(q) = *reinterpret_cast<const uint4 *>(from + at);
         });
     else if (bytes == 4)
-        pieces<kRun, 4 / sizeof(T)>(p, st, steps, s.width, [&](T *q, int at) {
+        pieces<T, kRun, 4 / sizeof(T)>(p, st, steps, s.width, [&](T *q, int at) {
             *reinterpret_cast<uint32_t *>(q) = *reinterpret_cast<const uint32_t *>(from + at);
         });
     else
-        pieces<kRun, 1>(p, st, steps, s.width, [&](T *q, int at) { *q = from[at]; });
+        pieces<T, kRun, 1>(p, st, steps, s.width, [&](T *q, int at) { *q = from[at]; });
 }
 
 // Steps past the sequence's end change nothing: gates of 1, values and
 // gradients of 0.
-template <class T, int kRun, int kArrays>
-__device__ __forceinline__ void pad(T *tile, int steps)
+template <class T, int kRun>
+__device__ __noinline__ void pad(T *tile, int steps, int arrays)
 {
     constexpr int kSteps = kRun * kRuns;
     for (int k = steps * kSlab + threadIdx.x; k < kSteps * kSlab; k += kThreads) {
-        tile[k] = from_f32<T>(INFINITY);
-#pragma unroll
-        for (int array = 1; array < kArrays; ++array)
-            tile[array * kSteps * kSlab + k] = from_f32<T>(0.0f);
+        const int at = place_of<T, kRun>(k / kSlab, k % kSlab);
+        tile[at] = from_f32<T>(INFINITY);
+        for (int array = 1; array < arrays; ++array)
+            tile[array * kSteps * kSlab + at] = from_f32<T>(0.0f);
     }
 }
 
@@ -347,10 +340,14 @@ __device__ __forceinline__ uint32_t resets_of(const Args &a, const Item &s, int6
     const int lane = threadIdx.x & 31, run = lane >> 2;
     if (s.b0 >= 0) {  // one sequence: the chunk's steps a lane each, four times over
         const uint8_t *p = a.reset + (t0 + lane) * a.rt + s.b0 * a.rb;
+        uint8_t begins[kRun * kRuns / 32];
+#pragma unroll
+        for (int q = 0; q < kRun * kRuns / 32; ++q)
+            begins[q] = 32 * q + lane < steps ? p[32 * q * a.rt] : 0;
         uint32_t mine = 0;
 #pragma unroll
         for (int q = 0; q < kRun * kRuns / 32; ++q) {
-            const uint32_t m = __ballot_sync(~0u, 32 * q + lane < steps && p[32 * q * a.rt] != 0);
+            const uint32_t m = __ballot_sync(~0u, begins[q] != 0);
             mine = run * kRun / 32 == q ? m >> (run * kRun % 32) : mine;
         }
         mine &= (1u << kRun) - 1;
@@ -369,162 +366,40 @@ __device__ __forceinline__ uint32_t resets_of(const Args &a, const Item &s, int6
     return m;
 }
 
-// The state at the start of the chunk at `place` of its chain from the chunks
-// before it, and the chunk's own map, `total`, for those after; by each warp
-// for its channels.
-__device__ void chained(const Args &a, const Item &t, const Map2 &total, int channel, float (&state)[2])
-{
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane & 3;
-    const uint32_t place = t.place, group = place / kGroup, groups = (a.chunks + kGroup - 1) / kGroup;
-    const int before = (int)(place % kGroup);
-    const int64_t chain = (int64_t)t.slab * kWarps + warp;
-    int *ready = a.ready + chain * a.chunks, *group_ready = a.group_ready + chain * groups;
-    float4 *maps = reinterpret_cast<float4 *>(a.maps + chain * a.chunks * 4);
-    float2 *group_state = a.group_state + chain * groups * 4;
-    if (lane < 4) {
-        __stcg(&maps[(int64_t)place * 4 + pair], make_float4(total.A[0], total.A[1], total.H[0], total.H[1]));
-        __threadfence();
+// A run's values in shared memory: array 0 holds gates (then h or their
+// gradients), 1 values (their gradients), 2 dh.
+template <class T, int kRun>
+struct Tile {
+    T *p;
+    __device__ __forceinline__ float2 get(int array, int k) const
+    {
+        return read2(p + array * (kRun * kRuns * kSlab) + k * step_of<T>());
     }
-    __syncwarp();
-    if (lane == 0)
-        store_flag(ready + place);
-    // a flag a lane: the chunks before this one in its group, and the group before
-    bool here = true;
-    if (lane < before)
-        here = wait_flag(ready + (int64_t)group * kGroup + lane, a.limit_ns);
-    if (lane == 31 && group > 0)
-        here = wait_flag(group_ready + group - 1, a.limit_ns);
-    here = __all_sync(~0u, here);
-    // four chunks a run of lanes, composed in order, then joined as runs are
-    Map2 m = identity();
-#pragma unroll
-    for (int k = 0; k < kGroup / kRuns; ++k) {
-        const int c = (lane >> 2) * (kGroup / kRuns) + k;
-        if (c < before) {
-            const float4 q = __ldcg(&maps[((int64_t)group * kGroup + c) * 4 + pair]);
-            m = then2(m, Map2{{q.x, q.y}, {q.z, q.w}});
-        }
+    __device__ __forceinline__ void put(int array, int k, float2 v) const
+    {
+        write2(p + array * (kRun * kRuns * kSlab) + k * step_of<T>(), v);
     }
-    m = whole<false>(joined<false>(m));
-    float2 start = make_float2(0.0f, 0.0f);
-    if (group > 0) {
-        start = __ldcg(&group_state[(int64_t)(group - 1) * 4 + pair]);
-    } else if (a.first) {
-        start.x = channel < t.width ? a.first[t.c + channel] : 0.0f;
-        start.y = channel + 1 < t.width ? a.first[t.c + channel + 1] : 0.0f;
-    }
-    // (past a wait that ran out all is NaN, so that no wrong state passes for a right one)
-    state[0] = here ? apply(m.A[0], m.H[0], start.x) : __int_as_float(0x7fffffff);
-    state[1] = here ? apply(m.A[1], m.H[1], start.y) : __int_as_float(0x7fffffff);
-    if (before == kGroup - 1) {
-        if (lane < 4) {
-            __stcg(&group_state[(int64_t)group * 4 + pair], make_float2(apply(total.A[0], total.H[0], state[0]),
-                                                                     apply(total.A[1], total.H[1], state[1])));
-            __threadfence();
-        }
-        __syncwarp();
-        if (lane == 0)
-            store_flag(group_ready + group);
-    }
-}
+};
 
-// Blocks of an SM: as many as registers and shared memory hold.
-__host__ __device__ constexpr int blocks_of(int e, bool back, int run)
-{
-    return run == kLongRun ? 2 : run == 4 || e == 2 ? 4 : back ? 2 : 3;
-}
+// A run's steps in a lane's registers.
+template <bool kBack, int kRun>
+struct Run {
+    uint32_t resets;  // steps that begin an episode, as resets_of gives them
+    bool plain;       // none in the warp: steps take no test for one
+    // the gate, its sign set where an episode begins; 1 - gate (backward) or (1 - gate) v
+    float2 ga[kRun], zb[kRun];
 
-// kBack: chunks from the last to the first.  What flows to before step t is
-// m_t = a_t k_t l_t, l_t = dh_t + m_{t+1}: a run's map of it has the forward
-// map's factor.
-// kDealt: places are drawn.  The next one is drawn while a chunk's maps are
-// made and fetched while its state is waited for, no sooner: a block that sat
-// on places would keep those after them waiting.
-template <class T, bool kBack, bool kDealt, int kStages, int kRun>
-__global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void scan_kernel(const Args a)
-{
-    constexpr int kArrays = kBack ? 3 : 2, kChunk = kRun * kRuns, kTile = kChunk * kSlab;
-    constexpr int kAhead = kDealt ? 1 : kStages - 1;  // chunks fetched before the first is taken
-    extern __shared__ __align__(128) uint8_t raw[];
-    __shared__ Item items[4];
-    T *tiles = reinterpret_cast<T *>(raw);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, run = lane >> 2;
-    const int channel = warp * 8 + 2 * (lane & 3);
-    const int spot = place_of<kRun>(run * kRun, channel);  // of the run's first step; steps are 64 apart
-
-    auto time_of = [&](const Item &t) { return (int64_t)(kBack ? a.chunks - 1 - t.place : t.place) * kChunk; };
-    auto steps_at = [&](int64_t t0) { return (int)(a.T - t0 < kChunk ? a.T - t0 : kChunk); };
-    auto fill = [&](uint32_t i) {
-        const Item &t = items[i & 3];
-        if (t.width > 0) {
-            const int64_t t0 = time_of(t);
-            const int steps = steps_at(t0);
-#pragma unroll
-            for (int k = 0; k < kArrays; ++k)
-                bring<T, kRun>(tiles + (int)(i % kStages * kArrays + k) * kTile, a.in[k], a.it[k], a.ib[k], t, t0, steps,
-                               a.in_bytes);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    // thread 0: the item after the one it set before
-    uint32_t slab_next = blockIdx.x, place_next = 0;
-    auto advance = [&](uint32_t i) {
-        if (kDealt) {
-            const uint32_t drawn = (uint32_t)atomicAdd(a.ticket, 1);
-            set_item(a, items[i & 3], drawn % a.slabs, drawn / a.slabs, drawn / a.slabs < a.chunks);
-        } else {
-            set_item(a, items[i & 3], slab_next, place_next, slab_next < a.slabs);
-            if (++place_next == a.chunks) {
-                place_next = 0;
-                slab_next += gridDim.x;
-            }
-        }
-    };
-
-    if (threadIdx.x == 0)
-        for (int i = 0; i <= kAhead - (kDealt ? 1 : 0); ++i)
-            advance(i);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        fill(i);
-    float carry[2] = {};  // walking: the state that enters the next chunk, in every run's lanes
-    for (uint32_t i = 0;; ++i) {
-        if (items[i & 3].width == 0)
-            break;
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-        __syncthreads();  // this chunk is here, the one before is done with
-        if (!kDealt)
-            fill(i + kAhead);
-        if (threadIdx.x == 0)
-            advance(i + kAhead + (kDealt ? 0 : 1));
-        const Item item = items[i & 3];
-        const int64_t t0 = time_of(item);
-        const int steps = steps_at(t0);
-        const bool first = channel < item.width, second = channel + 1 < item.width;
-        float *kept = a.states ? a.states + t0 / kChunk * (a.B * a.D) + item.c + channel : nullptr;
-        T *tile = tiles + (int)(i % kStages) * kArrays * kTile + spot;
-        if (steps < kChunk) {
-            pad<T, kRun, kArrays>(tiles + (int)(i % kStages) * kArrays * kTile, steps);
-            __syncthreads();
-        }
-        const uint32_t resets = resets_of<kRun>(a, item, t0, steps);
-        // (chunks without a reset take no test for one)
-        const bool plain = __all_sync(~0u, resets == 0);
-        float2 s = make_float2(0.0f, 0.0f);  // forward state before this lane's run
-        if (kBack) {
-            s.x = first ? kept[0] : 0.0f;
-            s.y = second ? kept[1] : 0.0f;
-        }
-        // the gate, its sign set where an episode begins; 1 - gate (backward) or (1 - gate) v
-        float2 ga[kRun], zb[kRun];
-        float2 A = make_float2(1.0f, 1.0f), H = make_float2(0.0f, 0.0f), Q = H;
-        auto gates = [&](auto simple) {
+    // Fills ga and zb; the run's map of the state.
+    template <class Tile>
+    __device__ __forceinline__ Map2 gates(const Tile &tile)
+    {
+        float2 A = make_float2(1.0f, 1.0f), H = make_float2(0.0f, 0.0f);
+        auto go = [&](auto simple) {
 #pragma unroll
             for (int k = 0; k < kRun; ++k) {
                 float2 z;
-                gates_of(read2(tile + k * kSlab), ga[k], z);
-                const float2 b = mul2(z, read2(tile + kTile + k * kSlab));
+                gates_of(tile.get(0, k), ga[k], z);
+                const float2 b = mul2(z, tile.get(1, k));
                 zb[k] = kBack ? z : b;
                 A = mul2(A, ga[k]);
                 if (simple.value) {
@@ -536,131 +411,483 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void s
             }
         };
         if (plain)
-            gates(std::true_type());
+            go(std::true_type());
         else
-            gates(std::false_type());
-        if (resets & 0xffffu)
-            A.x = -0.0f;
-        if (resets >> 16)
-            A.y = -0.0f;
-        Map2 m{{A.x, A.y}, {H.x, H.y}}, q = m;  // q, backward: of what flows back
-        if (kBack) {
-            auto flows = [&](auto simple) {
+            go(std::false_type());
+        return {{resets & 0xffffu ? -0.0f : A.x, resets >> 16 ? -0.0f : A.y}, {H.x, H.y}};
+    }
+
+    // Backward, after gates: the run's map of what flows back, its factors those of `map`.
+    template <class Tile>
+    __device__ __forceinline__ Map2 flows(const Tile &tile, const Map2 &map) const
+    {
+        float2 Q = make_float2(0.0f, 0.0f);
+        auto go = [&](auto simple) {
 #pragma unroll
-                for (int k = kRun - 1; k >= 0; --k) {
-                    Q = mul2(ga[k], add2(read2(tile + 2 * kTile + k * kSlab), Q));
-                    if (!simple.value) {
-                        Q.x = marked(ga[k].x) ? 0.0f : Q.x;
-                        Q.y = marked(ga[k].y) ? 0.0f : Q.y;
-                    }
+            for (int k = kRun - 1; k >= 0; --k) {
+                Q = mul2(ga[k], add2(tile.get(2, k), Q));
+                if (!simple.value) {
+                    Q.x = marked(ga[k].x) ? 0.0f : Q.x;
+                    Q.y = marked(ga[k].y) ? 0.0f : Q.y;
                 }
-            };
-            if (plain)
-                flows(std::true_type());
-            else
-                flows(std::false_type());
-            q.H[0] = Q.x;
-            q.H[1] = Q.y;
-            q = joined<true>(q);
-        }
-        m = joined<false>(m);
-        // what enters the chunk, of the chained direction
-        const Map2 total = kBack ? whole<true>(q) : whole<false>(m);
-        float in[2];
-        if (kDealt) {
-            __syncthreads();  // (the next item has been drawn)
-            fill(i + 1);
-            chained(a, item, total, channel, in);
-        } else if (item.place == 0) {
-            in[0] = a.first && first ? a.first[item.c + channel] : 0.0f;
-            in[1] = a.first && second ? a.first[item.c + channel + 1] : 0.0f;
-        } else {
-            in[0] = carry[0];
-            in[1] = carry[1];
-        }
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-            carry[v] = apply(total.A[v], total.H[v], in[v]);
-        if (a.last && item.place == a.chunks - 1 && run == 0) {
-            if (first)
-                a.last[item.c + channel] = carry[0];
-            if (second)
-                a.last[item.c + channel + 1] = carry[1];
-        }
-        if (!kBack) {
-            if (kept && run == 0) {
-                if (first)
-                    kept[0] = in[0];
-                if (second)
-                    kept[1] = in[1];
             }
-            s = make_float2(in[0], in[1]);
-        }
-        const Map2 pre = before_each<false>(m);
-        s.x = apply(pre.A[0], pre.H[0], s.x);
-        s.y = apply(pre.A[1], pre.H[1], s.y);
-        if (!kBack) {
-            auto states = [&](auto simple) {
+        };
+        if (plain)
+            go(std::true_type());
+        else
+            go(std::false_type());
+        return {{map.A[0], map.A[1]}, {Q.x, Q.y}};
+    }
+
+    // Backward, alone: the map of what flows back, without values.
+    template <class Tile>
+    __device__ __forceinline__ Map2 flow_map(const Tile &tile) const
+    {
+        float2 A = make_float2(1.0f, 1.0f), Q = make_float2(0.0f, 0.0f);
 #pragma unroll
-                for (int k = 0; k < kRun; ++k) {
-                    s = simple.value ? fma2(ga[k], s, zb[k])
-                                     : make_float2(apply(ga[k].x, zb[k].x, s.x), apply(ga[k].y, zb[k].y, s.y));
-                    write2(tile + k * kSlab, s);
+        for (int k = kRun - 1; k >= 0; --k) {
+            float2 g, z;
+            gates_of(tile.get(0, k), g, z);
+            A = mul2(A, g);
+            Q = mul2(g, add2(tile.get(1, k), Q));
+            Q.x = resets >> k & 1 ? 0.0f : Q.x;
+            Q.y = resets >> (16 + k) & 1 ? 0.0f : Q.y;
+        }
+        return {{resets & 0xffffu ? -0.0f : A.x, resets >> 16 ? -0.0f : A.y}, {Q.x, Q.y}};
+    }
+
+    // Forward: the states, to the gates' places; s is the one before the run.
+    template <class Tile>
+    __device__ __forceinline__ void states(const Tile &tile, float2 s) const
+    {
+        auto go = [&](auto simple) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                s = simple.value ? fma2(ga[k], s, zb[k])
+                                 : make_float2(apply(ga[k].x, zb[k].x, s.x), apply(ga[k].y, zb[k].y, s.y));
+                tile.put(0, k, s);
+            }
+        };
+        if (plain)
+            go(std::true_type());
+        else
+            go(std::false_type());
+    }
+
+    // Backward: the gradients, to the gates' and the values' places; f flows
+    // into the run from behind.
+    template <class Tile>
+    __device__ __forceinline__ void gradients(const Tile &tile, float2 s, float2 f) const
+    {
+        float2 u[kRun];  // v_t - k h_{t-1}
+        const float2 minus = make_float2(-1.0f, -1.0f);
+        auto go = [&](auto simple) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                const float2 x = tile.get(1, k);
+                float2 r = ga[k];
+                if (!simple.value) {
+                    s.x = marked(r.x) ? 0.0f : s.x;
+                    s.y = marked(r.y) ? 0.0f : s.y;
+                    r = make_float2(fabsf(r.x), fabsf(r.y));
                 }
-            };
-            if (plain)
-                states(std::true_type());
-            else
-                states(std::false_type());
+                u[k] = fma2(s, minus, x);
+                s = fma2(r, s, mul2(zb[k], x));
+            }
+#pragma unroll
+            for (int k = kRun - 1; k >= 0; --k) {
+                const float2 l = add2(tile.get(2, k), f), dv = mul2(zb[k], l);
+                f = mul2(ga[k], l);
+                tile.put(1, k, dv);
+                // (f is a l, or -a l where an episode begins)
+                float2 dg = mul2(mul2(f, zb[k]), u[k]);
+                if (simple.value) {
+                    dg = mul2(dg, minus);
+                } else {
+                    dg.x = marked(ga[k].x) ? dg.x : -dg.x;
+                    dg.y = marked(ga[k].y) ? dg.y : -dg.y;
+                    f.x = marked(ga[k].x) ? 0.0f : f.x;
+                    f.y = marked(ga[k].y) ? 0.0f : f.y;
+                }
+                tile.put(0, k, dg);
+            }
+        };
+        if (plain)
+            go(std::true_type());
+        else
+            go(std::false_type());
+    }
+};
+
+// A block's view of a chunk.
+struct Chunk {
+    int64_t t0;
+    uint32_t index;
+    int steps;
+    bool first, second;  // whether the lane's two channels are there
+    __device__ __forceinline__ float *kept(const Args &a, const Item &t, int channel) const
+    {
+        return a.states + index * (a.B * a.D) + t.c + channel;
+    }
+};
+template <bool kBack, int kSteps>
+__device__ __forceinline__ Chunk chunk_of(const Args &a, const Item &t, int channel)
+{
+    Chunk c;
+    c.index = kBack ? a.chunks - 1 - t.place : t.place;
+    c.t0 = (int64_t)c.index * kSteps;
+    c.steps = (int)(a.T - c.t0 < kSteps ? a.T - c.t0 : kSteps);
+    c.first = channel < t.width;
+    c.second = channel + 1 < t.width;
+    return c;
+}
+
+// The state that enters a segment: the first one through the maps of the
+// segments before it, eight lanes' shares of them in order.
+__device__ __noinline__ float2 entering(const Args &a, const Item &t, int channel)
+{
+    const int lane = threadIdx.x & 31, run = lane >> 2, pair = (threadIdx.x >> 5) * 4 + (lane & 3);
+    float2 s = make_float2(0.0f, 0.0f);
+    if (a.first) {
+        s.x = channel < t.width ? a.first[t.c + channel] : 0.0f;
+        s.y = channel + 1 < t.width ? a.first[t.c + channel + 1] : 0.0f;
+    }
+    if (t.segment == 0)
+        return s;
+    const float4 *maps = reinterpret_cast<const float4 *>(a.maps + (int64_t)t.slab * a.segments * kMaps + pair);
+    const uint32_t share = (t.segment + kRuns - 1) / kRuns;
+    Map2 m = identity();
+#pragma unroll 4
+    for (uint32_t k = run * share; k < (run + 1) * share && k < t.segment; ++k) {
+        const float4 q = maps[(int64_t)k * kMaps];
+        m = then2(m, Map2{{q.x, q.y}, {q.z, q.w}});
+    }
+    m = whole<false>(joined<false>(m));
+    return make_float2(apply(m.A[0], m.H[0], s.x), apply(m.A[1], m.H[1], s.y));
+}
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int c, int run, int b, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(map), "r"(c), "r"(run), "r"(0), "r"(b), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int c, int run, int b)
+{
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map),
+                 "r"(src), "r"(c), "r"(run), "r"(0), "r"(b)
+                 : "memory");
+}
+
+// Blocks of an SM: as many as registers and shared memory hold.
+__host__ __device__ constexpr int blocks_of(int e, bool back, int run)
+{
+    return run == kLongRun ? 2 : run == 4 || e == 2 ? 4 : back ? 2 : 3;
+}
+// Chunks in shared memory: the one that is taken and the next; forward also
+// one whose results are leaving.
+__host__ __device__ constexpr int stages_of(bool back, bool maps_only) { return back || maps_only ? 2 : 3; }
+
+// kBack: chunks from the last to the first.  What flows to before step t is
+// m_t = a_t k_t l_t, l_t = dh_t + m_{t+1}: a run's map of it has the forward
+// map's factor.
+// kMapsOnly: no outputs but the segments' maps (backward these take gates and
+// dh alone).
+template <class T, bool kBack, bool kMapsOnly, bool kTma, int kRun>
+__global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void walk_kernel(
+    const __grid_constant__ TensorMaps tma, const Args a)
+{
+    constexpr int kArrays = kBack && !kMapsOnly ? 3 : 2, kOut = kMapsOnly ? 0 : kBack ? 2 : 1;
+    constexpr int kChunk = kRun * kRuns, kTile = kChunk * kSlab, kStages = stages_of(kBack, kMapsOnly);
+    constexpr int kBoxes = sizeof(T) / 2, kBox = kTile / kBoxes;  // of an array's chunk; values of one
+    extern __shared__ uint8_t raw[];
+    __shared__ Item items[4];
+    __shared__ uint64_t bars[kStages];
+    __shared__ int dead;
+    T *tiles = reinterpret_cast<T *>(raw + ((1024 - (smem_addr(raw) & 1023)) & 1023));
+    const int channel = (threadIdx.x >> 5) * 8 + 2 * (threadIdx.x & 3);
+    const int spot = place_of<T, kRun>((threadIdx.x & 31) / 4 * kRun, channel);  // of the run's first step
+    auto stage = [&](int s) { return tiles + s * kArrays * kTile; };
+    // which of the call's arrays the k-th of the tile is
+    auto array_of = [](int k) { return kBack && kMapsOnly && k == 1 ? 2 : k; };
+    auto by_tma = [&](const Item &t) {
+        const int64_t t0 = (int64_t)(kBack ? a.chunks - 1 - t.place : t.place) * kChunk;
+        return kTma && a.T - t0 >= kChunk;
+    };
+    // all threads: an item's chunk to stage s
+    auto fill = [&](const Item &t, int s) {
+        if (t.width > 0) {
+            const int64_t t0 = (int64_t)(kBack ? a.chunks - 1 - t.place : t.place) * kChunk;
+            if (by_tma(t)) {
+                if (threadIdx.x == 0) {
+                    // (what left from this stage has been read)
+                    if constexpr (kOut > 0)
+                        asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStages - 2) : "memory");
+                    const uint32_t bar = smem_addr(bars + s);
+                    bar_expect(bar, kArrays * kTile * sizeof(T));
+#pragma unroll
+                    for (int k = 0; k < kArrays; ++k)
+#pragma unroll
+                        for (int q = 0; q < kBoxes; ++q)
+                            tma_load(smem_addr(stage(s) + k * kTile + q * kBox), &tma.in[array_of(k)],
+                                     (int)t.d + q * (kSlab / kBoxes), (int)(t0 / kRun), (int)t.b, bar);
+                }
+            } else {
+                if (kTma && kOut > 0) {
+                    if (threadIdx.x == 0)
+                        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncthreads();
+                }
+                const int steps = (int)(a.T - t0 < kChunk ? a.T - t0 : kChunk);
+#pragma unroll
+                for (int k = 0; k < kArrays; ++k) {
+                    const int q = array_of(k);
+                    bring<T, kRun>(stage(s) + k * kTile, a.in[q], a.it[q], a.ib[q], t, t0, steps, a.in_bytes);
+                }
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    Order order{blockIdx.x, 0, 0};  // thread 0's
+    if (threadIdx.x == 0) {
+        dead = 0;
+        for (int s = 0; s < kStages; ++s)
+            bar_init(smem_addr(bars + s), 1);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        order.open(a);
+        order.next(a, items[0]);
+        order.next(a, items[1]);
+    }
+    __syncthreads();
+    fill(items[0], 0);
+    bool ok = true;
+    uint32_t phases = 0;
+    Map2 all = identity();     // the segment's map so far
+    float carry[2] = {};       // the state that enters the next chunk, in every run's lanes
+    int s = 0;
+    for (uint32_t i = 0; items[i & 3].width > 0; ++i) {
+        if (by_tma(items[i & 3])) {
+            ok = ok && bar_wait(smem_addr(bars + s), phases >> s & 1, &dead);
+            phases ^= 1u << s;
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();  // this chunk is here, the one before is done with
+        const int s_next = s + 1 == kStages ? 0 : s + 1;
+        fill(items[(i + 1) & 3], s_next);
+        if (threadIdx.x == 0)
+            order.next(a, items[(i + 2) & 3]);
+        const Item item = items[i & 3];
+        const Chunk c = chunk_of<kBack, kChunk>(a, item, channel);
+        if (c.steps < kChunk) {
+            pad<T, kRun>(stage(s), c.steps, kArrays);
+            __syncthreads();
+        }
+        const Tile<T, kRun> tile{stage(s) + spot};
+        Run<kBack, kRun> run;
+        run.resets = resets_of<kRun>(a, item, c.t0, c.steps);
+        run.plain = __all_sync(~0u, run.resets == 0);
+        if constexpr (kMapsOnly) {
+            const Map2 m = kBack ? whole<true>(joined<true>(run.flow_map(tile))) : whole<false>(joined<false>(run.gates(tile)));
+            all = item.enters ? m : then2(all, m);
+            const uint32_t end = (item.segment + 1) * a.per;
+            if (item.place + 1 == (end < a.chunks ? end : a.chunks) && (threadIdx.x & 31) < 4) {
+                if (!ok)
+                    all = Map2{{-0.0f, -0.0f}, {__int_as_float(0x7fffffff), __int_as_float(0x7fffffff)}};
+                *reinterpret_cast<float4 *>(a.maps + ((int64_t)item.slab * a.segments + item.segment) * kMaps +
+                                            (threadIdx.x >> 5) * 4 + (threadIdx.x & 3)) =
+                    make_float4(all.A[0], all.A[1], all.H[0], all.H[1]);
+            }
         } else {
-            const Map2 post = before_each<true>(q);
-            // what flows into the run from behind
-            float2 f = make_float2(apply(post.A[0], post.H[0], in[0]), apply(post.A[1], post.H[1], in[1]));
-            float2 u[kRun];  // v_t - k h_{t-1}
-            const float2 minus = make_float2(-1.0f, -1.0f);
-            auto gradients = [&](auto simple) {
-#pragma unroll
-                for (int k = 0; k < kRun; ++k) {
-                    const float2 x = read2(tile + kTile + k * kSlab);
-                    float2 r = ga[k];
-                    if (!simple.value) {
-                        s.x = marked(r.x) ? 0.0f : s.x;
-                        s.y = marked(r.y) ? 0.0f : s.y;
-                        r = make_float2(fabsf(r.x), fabsf(r.y));
-                    }
-                    u[k] = fma2(s, minus, x);
-                    s = fma2(r, s, mul2(zb[k], x));
+            Map2 m = run.gates(tile), pre, post, total;
+            if (kBack) {
+                const Map2 q = joined<true>(run.flows(tile, m));
+                post = before_each<true>(q);
+                total = whole<true>(q);
+                pre = before_each<false>(joined<false>(m));
+            } else {
+                m = joined<false>(m);
+                pre = before_each<false>(m);
+                total = whole<false>(m);
+            }
+            if (item.enters) {
+                const float2 v = entering(a, items[i & 3], channel);
+                carry[0] = v.x;
+                carry[1] = v.y;
+            }
+            if (!ok)  // (past a wait that ran out: no wrong state passes for a right one)
+                carry[0] = carry[1] = __int_as_float(0x7fffffff);
+            const bool speaks = (threadIdx.x & 31) < 4;  // one run's lanes for all
+            float2 h;
+            if (kBack) {
+                const float *kept = c.kept(a, item, channel);
+                h = make_float2(c.first ? kept[0] : 0.0f, c.second ? kept[1] : 0.0f);
+            } else {
+                h = make_float2(carry[0], carry[1]);
+                if (a.states && speaks) {
+                    float *kept = c.kept(a, item, channel);
+                    if (c.first)
+                        kept[0] = h.x;
+                    if (c.second)
+                        kept[1] = h.y;
                 }
-#pragma unroll
-                for (int k = kRun - 1; k >= 0; --k) {
-                    const float2 l = add2(read2(tile + 2 * kTile + k * kSlab), f), dv = mul2(zb[k], l);
-                    f = mul2(ga[k], l);
-                    write2(tile + kTile + k * kSlab, dv);
-                    // (f is a l, or -a l where an episode begins)
-                    float2 dg = mul2(mul2(f, zb[k]), u[k]);
-                    if (simple.value) {
-                        dg = mul2(dg, minus);
-                    } else {
-                        dg.x = marked(ga[k].x) ? dg.x : -dg.x;
-                        dg.y = marked(ga[k].y) ? dg.y : -dg.y;
-                        f.x = marked(ga[k].x) ? 0.0f : f.x;
-                        f.y = marked(ga[k].y) ? 0.0f : f.y;
-                    }
-                    write2(tile + k * kSlab, dg);
-                }
-            };
-            if (plain)
-                gradients(std::true_type());
+            }
+            h = make_float2(apply(pre.A[0], pre.H[0], h.x), apply(pre.A[1], pre.H[1], h.y));
+            if (kBack)
+                run.gradients(tile, h, make_float2(apply(post.A[0], post.H[0], carry[0]), apply(post.A[1], post.H[1], carry[1])));
             else
-                gradients(std::false_type());
-        }
-        __syncthreads();
-        const T *done = tiles + (int)(i % kStages) * kArrays * kTile;
+                run.states(tile, h);
+            carry[0] = apply(total.A[0], total.H[0], carry[0]);
+            carry[1] = apply(total.A[1], total.H[1], carry[1]);
+            if (a.last && item.place == a.chunks - 1 && speaks) {
+                if (c.first)
+                    a.last[item.c + channel] = carry[0];
+                if (c.second)
+                    a.last[item.c + channel + 1] = carry[1];
+            }
+            const bool out_tma = by_tma(item);
+            if (out_tma)
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncthreads();
+            if (out_tma) {
+                if (threadIdx.x == 0) {
 #pragma unroll
-        for (int k = 0; k < (kBack ? 2 : 1); ++k)
-            take_out<T, kRun>(done + k * kTile, a.out[k], a.ot[k], a.ob[k], item, t0, steps, a.out_bytes);
+                    for (int k = 0; k < kOut; ++k)
+#pragma unroll
+                        for (int q = 0; q < kBoxes; ++q)
+                            if (q * (kSlab / kBoxes) < item.width)
+                                tma_store(&tma.out[k], smem_addr(stage(s) + k * kTile + q * kBox),
+                                          (int)item.d + q * (kSlab / kBoxes), (int)(c.t0 / kRun), (int)item.b);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kOut; ++k)
+                    take_out<T, kRun>(stage(s) + k * kTile, a.out[k], a.ot[k], a.ob[k], items[i & 3], c.t0, c.steps,
+                                      a.out_bytes);
+            }
+            if (kTma && threadIdx.x == 0)
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        s = s_next;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (kTma && kOut > 0 && threadIdx.x == 0)
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (!ok)
+        linger();
+}
+
+// The values of a thread's two channels, all steps in registers.
+template <class T, int kRun, int kArrays>
+struct Column {
+    T *p[kArrays][2];        // where step 0 of either channel is
+    int64_t stride[kArrays];
+    void *out[2][2];
+    int64_t out_stride[2];
+    int steps;
+    bool pairs, both;        // neighbours in one access; whether there is a second
+    T v[kArrays][kRun][2];
+
+    __device__ __forceinline__ void load()
+    {
+#pragma unroll
+        for (int q = 0; q < kArrays; ++q) {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                v[q][k][0] = v[q][k][1] = from_f32<T>(q == 0 ? INFINITY : 0.0f);
+                if (k >= steps)
+                    continue;
+                const T *at = p[q][0] + k * stride[q];
+                if (pairs) {
+                    if constexpr (sizeof(T) == 4)
+                        *reinterpret_cast<float2 *>(v[q][k]) = *reinterpret_cast<const float2 *>(at);
+                    else
+                        *reinterpret_cast<uint32_t *>(v[q][k]) = *reinterpret_cast<const uint32_t *>(at);
+                } else {
+                    v[q][k][0] = *at;
+                    if (both)
+                        v[q][k][1] = p[q][1][k * stride[q]];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float2 get(int array, int k) const
+    {
+        return make_float2(to_f32(v[array][k][0]), to_f32(v[array][k][1]));
+    }
+    __device__ __forceinline__ void put(int array, int k, float2 x) const
+    {
+        if (k >= steps)
+            return;
+        T *at = (T *)out[array][0] + k * out_stride[array];
+        if (pairs) {
+            write2(at, x);
+        } else {
+            *at = from_f32<T>(x.x);
+            if (both)
+                ((T *)out[array][1])[k * out_stride[array]] = from_f32<T>(x.y);
+        }
+    }
+};
+
+// Sequences of at most kRun steps: a thread takes two channels.
+template <class T, bool kBack, int kRun>
+__global__ __launch_bounds__(256) void brief_kernel(const Args a, bool pairs)
+{
+    constexpr int kArrays = kBack ? 3 : 2;
+    const int64_t n = a.B * a.D, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
+    if (c >= n)
+        return;
+    Column<T, kRun, kArrays> col;
+    col.pairs = pairs;
+    col.both = c + 1 < n;
+    col.steps = (int)a.T;
+    Run<kBack, kRun> run;
+    run.resets = 0;
+    float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        const int64_t cv = v && !col.both ? c : c + v, b = divide(cv, a.D), d = cv - b * a.D;
+#pragma unroll
+        for (int k = 0; k < kArrays; ++k) {
+            col.p[k][v] = (T *)a.in[k] + b * a.ib[k] + d;
+            col.stride[k] = a.it[k];
+        }
+#pragma unroll
+        for (int k = 0; k < (kBack ? 2 : 1); ++k) {
+            col.out[k][v] = (T *)a.out[k] + b * a.ob[k] + d;
+            col.out_stride[k] = a.ot[k];
+        }
+        if (a.reset)
+            for (int k = 0; k < col.steps; ++k)
+                run.resets |= (a.reset[k * a.rt + b * a.rb] != 0 ? 1u : 0u) << (16 * v + k);
+        const float *from = kBack ? a.states : a.first;
+        (v ? s.y : s.x) = from ? from[cv] : 0.0f;
+    }
+    run.plain = run.resets == 0;
+    col.load();
+    const Map2 m = run.gates(col);
+    float2 f = make_float2(0.0f, 0.0f);  // backward: what flows in from behind
+    if (kBack) {
+        if (a.first)
+            f = make_float2(a.first[c], a.first[col.both ? c + 1 : c]);
+        const Map2 q = run.flows(col, m);
+        run.gradients(col, s, f);
+        s = make_float2(apply(q.A[0], q.H[0], f.x), apply(q.A[1], q.H[1], f.y));
+    } else {
+        if (a.states) {
+            a.states[c] = s.x;
+            if (col.both)
+                a.states[c + 1] = s.y;
+        }
+        run.states(col, s);
+        s = make_float2(apply(m.A[0], m.H[0], s.x), apply(m.A[1], m.H[1], s.y));
+    }
+    if (a.last) {
+        a.last[c] = s.x;
+        if (col.both)
+            a.last[c + 1] = s.y;
+    }
 }
 
 // One step: every value once, kVec at a time.
@@ -730,31 +957,26 @@ int64_t chunks_of(int64_t T, int e) { return up(T, run_of(T, e) * kRuns); }
 // Blocks of channels: numbered through where the sequences lie side by side.
 int64_t slabs_of(int64_t B, int64_t D, bool flat) { return flat ? up(B * D, kSlab) : B * up(D, kSlab); }
 
-// Whether chunks are dealt out instead of walked: where walking would leave
-// blocks without channels, or the last round of them mostly empty.
-bool dealt(int64_t slabs, int64_t chunks, int64_t resident)
+// Segments of a sequence: one where the channels fill more than half of what
+// the GPU holds (cutting reads the inputs twice), else what fills it.
+int64_t segments_of(int64_t slabs, int64_t chunks, int64_t resident)
 {
-    if (chunks == 1)
-        return false;
-    const int64_t rounds = up(slabs, resident);
-    return rounds * resident * 8 > slabs * 9;
+    if (2 * slabs > resident || chunks <= 4)
+        return 1;
+    const int64_t most = resident / slabs, per = up(chunks, most < chunks ? most : chunks);
+    return up(chunks, per);
 }
 
-int64_t flag_bytes(int64_t slabs, int64_t chunks) { return up((1 + slabs * kWarps * (chunks + up(chunks, kGroup))) * 4, 256) * 256; }
-
-int64_t plan_bytes(int64_t slabs, int64_t chunks)
-{
-    return flag_bytes(slabs, chunks) + slabs * kWarps * 4 * (chunks * (int64_t)sizeof(Map2) + up(chunks, kGroup) * 8);
-}
+int64_t resident_of(int e, bool back, int run) { return (int64_t)kSms * blocks_of(e, back, run); }
 
 int64_t work_bytes(int64_t T, int64_t B, int64_t D, int e)
 {
-    const int64_t chunks = chunks_of(T, e);
     int64_t most = 0;
     for (int flat = 0; flat < 2; ++flat)
         for (int back = 0; back < 2; ++back) {
-            const int64_t slabs = slabs_of(B, D, flat);
-            const int64_t need = T > 1 && dealt(slabs, chunks, kSms * blocks_of(e, back, run_of(T, e))) ? plan_bytes(slabs, chunks) : 0;
+            const int64_t slabs = slabs_of(B, D, flat),
+                          n = segments_of(slabs, chunks_of(T, e), resident_of(e, back, run_of(T, e)));
+            const int64_t need = n > 1 ? slabs * n * kMaps * (int64_t)sizeof(Map2) : 0;
             most = need > most ? need : most;
         }
     return most;
@@ -771,70 +993,95 @@ int copy_bytes(int so_far, const void *p, int64_t t, int64_t b, int64_t n, int e
     return fits(16) ? 16 : fits(4) ? 4 : 0;
 }
 
-template <class T, bool kBack, int kRun>
-cudaError_t go(Args &a, void *work, cudaStream_t st)
+// An array for TMA: channels, runs, a run's steps, sequences.
+bool array_map(CUtensorMap *map, int dtype, const void *p, int64_t n, int64_t T, int run, int64_t st, int64_t B, int64_t sb)
 {
-    constexpr int kArrays = kBack ? 3 : 2, kOut = kBack ? 2 : 1, kStages = kBack || sizeof(T) == 4 ? 2 : 3;
-    constexpr int kBytes = kStages * kArrays * kRun * kRuns * kSlab * (int)sizeof(T);
-    const int64_t chunks = chunks_of(a.T, sizeof(T));
-    a.flat = true;
-    for (int k = 0; k < kArrays; ++k)
-        a.flat = a.flat && (a.B == 1 || a.ib[k] == a.D);
-    for (int k = 0; k < kOut; ++k)
-        a.flat = a.flat && (a.B == 1 || a.ob[k] == a.D);
-    const int64_t slabs = slabs_of(a.B, a.D, a.flat);
-    if (slabs * chunks > (int64_t(1) << 31))  // (beyond any memory)
+    const int64_t dims[4] = {n, T / run, run, B}, strides[3] = {run * st, st, B > 1 ? sb : run * st};
+    const int box[4] = {dtype == AV_F32 ? 32 : 64, kRuns, run, 1};
+    return make_map(map, dtype, p, 4, dims, strides, box);
+}
+
+template <class T, bool kBack, int kRun>
+cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
+{
+    constexpr int kArrays = kBack ? 3 : 2, kOut = kBack ? 2 : 1;
+    const int64_t chunks = chunks_of(a.T, sizeof(T)), slabs = slabs_of(a.B, a.D, a.flat);
+    const int64_t resident = resident_of(sizeof(T), kBack, kRun), segments = segments_of(slabs, chunks, resident);
+    if (slabs * segments > (int64_t(1) << 30) || chunks > (int64_t(1) << 30))  // (beyond any memory)
         return cudaErrorInvalidValue;
     a.slabs = (uint32_t)slabs;
     a.chunks = (uint32_t)chunks;
-    const int64_t n = a.flat ? a.B * a.D : a.D;
+    a.segments = (uint32_t)segments;
+    a.per = (uint32_t)up(chunks, segments);
+    a.maps = (Map2 *)work;
+    const int64_t n = a.flat ? a.B * a.D : a.D, sequences = a.flat ? 1 : a.B;
     a.in_bytes = a.out_bytes = 16;
     for (int k = 0; k < kArrays; ++k)
         a.in_bytes = copy_bytes(a.in_bytes, a.in[k], a.it[k], a.flat ? 0 : a.ib[k], n, sizeof(T));
     for (int k = 0; k < kOut; ++k)
         a.out_bytes = copy_bytes(a.out_bytes, a.out[k], a.ot[k], a.flat ? 0 : a.ob[k], n, sizeof(T));
-    constexpr int64_t resident = kSms * blocks_of(sizeof(T), kBack, kRun);
-    int64_t grid = slabs < resident ? slabs : resident;
-    if (dealt(slabs, chunks, resident)) {
-        const int64_t flags = flag_bytes(slabs, chunks), items = slabs * chunks;
-        grid = items < resident ? items : resident;
-        a.ticket = (int *)work;
-        a.ready = a.ticket + 1;
-        a.group_ready = a.ready + slabs * kWarps * chunks;
-        a.maps = (Map2 *)((char *)work + flags);
-        a.group_state = (float2 *)(a.maps + slabs * kWarps * chunks * 4);
-        a.limit_ns = 4000000000ll;
-        if (const char *ms = getenv("AV_SCAN_WAIT_MS"))  // for tests of the limit
-            a.limit_ns = atoll(ms) * 1000000;
-        const cudaError_t e = cudaMemsetAsync(work, 0, flags, st);
+    TensorMaps maps;
+    bool tma = a.in_bytes == 16 && a.out_bytes == 16 && a.T >= kRun * kRuns && n < (int64_t(1) << 31) &&
+               sequences < (int64_t(1) << 31);
+    for (int k = 0; k < kArrays && tma; ++k)
+        tma = array_map(&maps.in[k], dtype, a.in[k], n, a.T, kRun, a.it[k], sequences, a.ib[k]);
+    for (int k = 0; k < kOut && tma; ++k)
+        tma = array_map(&maps.out[k], dtype, a.out[k], n, a.T, kRun, a.ot[k], sequences, a.ob[k]);
+    const int64_t units = slabs * segments, grid = units < resident ? units : resident;
+    auto run = [&](auto kernel, int stages, int arrays) {
+        const int bytes = stages * arrays * kRun * kRuns * kSlab * (int)sizeof(T) + 1024;
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess)
             return e;
-    }
-    auto run = [&](auto kernel) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-        if (e != cudaSuccess)
-            return e;
-        kernel<<<(unsigned)grid, kThreads, kBytes, st>>>(a);
+        kernel<<<(unsigned)grid, kThreads, bytes, st>>>(maps, a);
         return cudaGetLastError();
     };
-    if constexpr (kRun == (sizeof(T) == 4 ? 8 : kLongRun)) {
-        if (a.ticket)
-            return run(scan_kernel<T, kBack, true, kStages, kRun>);
+    if (segments > 1) {
+        const int stages = stages_of(kBack, true);
+        const cudaError_t e = tma ? run(walk_kernel<T, kBack, true, true, kRun>, stages, 2)
+                                  : run(walk_kernel<T, kBack, true, false, kRun>, stages, 2);
+        if (e != cudaSuccess)
+            return e;
     }
-    return run(scan_kernel<T, kBack, false, kStages, kRun>);
+    const int stages = stages_of(kBack, false);
+    return tma ? run(walk_kernel<T, kBack, false, true, kRun>, stages, kArrays)
+               : run(walk_kernel<T, kBack, false, false, kRun>, stages, kArrays);
+}
+
+template <class T, bool kBack, int kRun>
+cudaError_t brief(const Args &a, cudaStream_t st)
+{
+    // neighbours in one access: even channels are of one sequence with the next, and all arrays keep them together
+    bool pairs = a.D % 2 == 0;
+    auto apart = [&](const void *p, int64_t t, int64_t b) {
+        pairs = pairs && (reinterpret_cast<uintptr_t>(p) & (2 * sizeof(T) - 1)) == 0 && t % 2 == 0 && b % 2 == 0;
+    };
+    for (int k = 0; k < (kBack ? 3 : 2); ++k)
+        apart(a.in[k], a.it[k], a.ib[k]);
+    for (int k = 0; k < (kBack ? 2 : 1); ++k)
+        apart(a.out[k], a.ot[k], a.ob[k]);
+    brief_kernel<T, kBack, kRun><<<(unsigned)up(a.B * a.D, 512), 256, 0, st>>>(a, pairs);
+    return cudaGetLastError();
 }
 
 template <bool kBack>
 cudaError_t launch(Args &a, int dtype, void *work, cudaStream_t st)
 {
+    a.flat = true;
+    for (int k = 0; k < (kBack ? 3 : 2); ++k)
+        a.flat = a.flat && (a.B == 1 || a.ib[k] == a.D);
+    for (int k = 0; k < (kBack ? 2 : 1); ++k)
+        a.flat = a.flat && (a.B == 1 || a.ob[k] == a.D);
     return with_type(dtype, [&](auto v) {
         using T = decltype(v);
+        if (a.T <= 16 && a.B * a.D >= kBriefChannels)
+            return a.T <= 4 ? brief<T, kBack, 4>(a, st) : a.T <= 8 ? brief<T, kBack, 8>(a, st) : brief<T, kBack, 16>(a, st);
         const int run = run_of(a.T, sizeof(T));
         if constexpr (sizeof(T) == 2) {
             if (run == kLongRun)
-                return go<T, kBack, kLongRun>(a, work, st);
+                return walk<T, kBack, kLongRun>(a, dtype, work, st);
         }
-        return run == 4 ? go<T, kBack, 4>(a, work, st) : go<T, kBack, 8>(a, work, st);
+        return run == 4 ? walk<T, kBack, 4>(a, dtype, work, st) : walk<T, kBack, 8>(a, dtype, work, st);
     });
 }
 
