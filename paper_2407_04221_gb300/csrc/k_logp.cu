@@ -30,8 +30,9 @@ constexpr int kTiny = 8;           // entries of a row that a thread takes
 constexpr int kTinyThreads = 128;
 constexpr int kNarrow = 1024;      // entries of a row that a group of lanes takes
 constexpr int kNarrowThreads = 256;
-constexpr int kWideThreads = 512;
-constexpr int kGradThreads = 256;  // of a block that takes a part of a row's gradient
+constexpr int kMiddle = 8192;      // entries of a row that a block of 128 threads takes; longer ones one of 512
+constexpr int kGradThreads = 256;
+constexpr int kGradWarp = 4096;    // entries of a row whose gradient a warp takes
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -164,7 +165,7 @@ struct Row {
     }
 };
 
-template <class F>
+template <int kWideThreads, class F>
 __device__ __forceinline__ float reduce(float v, float *slots, F f)
 {
 #pragma unroll
@@ -183,6 +184,7 @@ __device__ __forceinline__ float reduce(float v, float *slots, F f)
 
 constexpr int kListed = 512;  // candidates of a row
 
+template <int kWideThreads>
 struct Scratch {
     static constexpr int kWarps = kWideThreads / 32;
     float slots[kWarps];
@@ -194,8 +196,10 @@ struct Scratch {
 };
 
 // The k-th largest of the threads' values.
-__device__ uint32_t kth(uint32_t v, int k, Scratch &s)
+template <int kWideThreads>
+__device__ uint32_t kth(uint32_t v, int k, Scratch<kWideThreads> &s)
 {
+    constexpr int kWarps = kWideThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t last = 0;
     for (int i = 0; i < k; ++i) {
@@ -210,9 +214,9 @@ __device__ uint32_t kth(uint32_t v, int k, Scratch &s)
     if (warp == 0) {  // each warp's are in order: a lane holds the next of one
         int at = 0;
         for (int i = 0; i < k; ++i) {
-            const uint32_t u = lane < Scratch::kWarps && at < k ? s.heads[lane * AV_MAX_TOP + at] : 0;
+            const uint32_t u = lane < kWarps && at < k ? s.heads[lane * AV_MAX_TOP + at] : 0;
             last = __reduce_max_sync(~0u, u);
-            const uint32_t holders = __ballot_sync(~0u, u == last && lane < Scratch::kWarps);
+            const uint32_t holders = __ballot_sync(~0u, u == last && lane < kWarps);
             at += lane == __ffs(holders) - 1;
         }
         if (lane == 0) {
@@ -226,7 +230,7 @@ __device__ uint32_t kth(uint32_t v, int k, Scratch &s)
 
 // f(value, index) for the entries of the row that `thread` takes, seen by
 // thread `lane` of `lanes`.
-template <bool kMask, class T, class F>
+template <int kWideThreads, bool kMask, class T, class F>
 __device__ __forceinline__ void entries(const Row<T> &row, int thread, int lane, int lanes, F f)
 {
     for (int i = thread + lane * kWideThreads; i < row.loose(); i += lanes * kWideThreads)
@@ -240,13 +244,13 @@ __device__ __forceinline__ void entries(const Row<T> &row, int thread, int lane,
     }
 }
 
-template <class T, bool kMask, bool kTop>
+template <class T, int kWideThreads, bool kMask, bool kTop>
 __global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs a, int top, float *logp, float *entropy,
                                                                  float *peak, float *logz, float *top_logp,
                                                                  int32_t *top_index)
 {
     constexpr int kPack = Row<T>::kPack, kAhead = 4;
-    __shared__ Scratch s;
+    __shared__ Scratch<kWideThreads> s;
     const int thread = threadIdx.x;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const Row<T> row((const T *)a.logits + r * a.stride, kMask ? a.mask + r * a.mask_stride : nullptr, a.V);
@@ -274,10 +278,10 @@ __global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs 
             take(q, v);
         }
         const float mine = q.m;
-        const float m = reduce(mine, s.slots, [](float x, float y) { return fmaxf(x, y); });
+        const float m = reduce<kWideThreads>(mine, s.slots, [](float x, float y) { return fmaxf(x, y); });
         raise(q, m);
         auto plus = [](float x, float y) { return x + y; };
-        const float e = reduce(q.e.x + q.e.y, s.slots, plus), ex = reduce(q.ex.x + q.ex.y, s.slots, plus);
+        const float e = reduce<kWideThreads>(q.e.x + q.e.y, s.slots, plus), ex = reduce<kWideThreads>(q.ex.x + q.ex.y, s.slots, plus);
         const bool some = e != 0.0f;  // (NaN counts)
         const float z = some ? logf(e) : no_value();
         if (thread == 0) {
@@ -303,7 +307,7 @@ __global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs 
         while (again) {  // the warp looks at one thread's entries after another
             const int lane = __ffs(again) - 1;
             again &= again - 1;
-            entries<kMask>(row, (thread & ~31) + lane, thread & 31, 32, [&](float v, int j) {
+            entries<kWideThreads, kMask>(row, (thread & ~31) + lane, thread & 31, 32, [&](float v, int j) {
                 const uint32_t u = order_of(v);
                 if (u >= floor && u != 0) {
                     const int at = atomicAdd(&s.count, 1);
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs 
             uint64_t last = ~0ull;
             for (int k = 0; k < top; ++k) {
                 uint64_t best = 0;
-                entries<kMask>(row, thread, 0, 1, [&](float v, int j) {
+                entries<kWideThreads, kMask>(row, thread, 0, 1, [&](float v, int j) {
                     const uint64_t key = rank_key(v, j);
                     best = key < last && key > best ? key : best;
                 });
@@ -346,7 +350,7 @@ __global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs 
                 if ((thread & 31) == 0)
                     s.best[thread >> 5] = best;
                 __syncthreads();
-                for (int w = 0; w < Scratch::kWarps; ++w)
+                for (int w = 0; w < kWideThreads / 32; ++w)
                     best = s.best[w] > best ? s.best[w] : best;
                 last = best;
                 if (thread == 0) {
@@ -592,19 +596,21 @@ __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_grad_kernel(const 
     }
 }
 
-// A block takes a part of a row.
-template <class T, bool kMask>
+// A block takes a part of a row, or a warp a row.
+template <class T, int kLanes, bool kMask>
 __global__ __launch_bounds__(kGradThreads) void logp_wide_grad_kernel(const LogpArgs a, const float *dlogp,
                                                                       const float *dentropy, const float *peak,
                                                                       const float *logz, const float *entropy,
                                                                       T *dlogits, int64_t dstride, bool packed)
 {
     constexpr int kPack = Row<T>::kPack, kAhead = 4;
-    const int64_t r = blockIdx.x;
+    const int64_t r = (int64_t)blockIdx.x * (kGradThreads / kLanes) + threadIdx.x / kLanes;
+    if (r >= a.rows)
+        return;
     const Row<T> row((const T *)a.logits + r * a.stride, kMask ? a.mask + r * a.mask_stride : nullptr, a.V);
     const Slope s = slope_of(a, r, dlogp, dentropy, peak, logz, entropy);
     T *dx = dlogits + r * dstride;
-    const int thread = threadIdx.x + blockIdx.y * kGradThreads, step = kGradThreads * gridDim.y;
+    const int thread = threadIdx.x % kLanes + blockIdx.y * kLanes, step = kLanes * gridDim.y;
     if (!packed) {  // dlogits' rows begin elsewhere in 16 bytes than those of logits
         for (int j = thread; j < a.V; j += step)
             dx[j] = from_f32<T>(gradient_at<kMask>(s, row.template entry<kMask>(j), j));
@@ -727,10 +733,15 @@ cudaError_t launch_logp(const LogpArgs &a, int top, float *logp, float *entropy,
                 return;
             }
             with_flag(top > 0, [&](auto tops) {
-                const int64_t most = 152 * 4 * 4;
-                logp_wide_kernel<T, mask.value, tops.value>
-                    <<<(unsigned)(a.rows < most ? a.rows : most), kWideThreads, 0, st>>>(a, top, logp, entropy, peak,
-                                                                                      logz, top_logp, top_index);
+                auto run = [&](auto kernel, int threads) {
+                    const int64_t most = 152 * 4 * (2048 / threads);
+                    kernel<<<(unsigned)(a.rows < most ? a.rows : most), threads, 0, st>>>(a, top, logp, entropy, peak,
+                                                                                         logz, top_logp, top_index);
+                };
+                if (a.V <= kMiddle && a.rows >= 152)
+                    run(logp_wide_kernel<T, 128, mask.value, tops.value>, 128);
+                else
+                    run(logp_wide_kernel<T, 512, mask.value, tops.value>, 512);
             });
         });
     });
@@ -765,9 +776,13 @@ cudaError_t launch_logp_grad(const LogpArgs &a, const float *dlogp, const float 
             if (a.V <= kTiny) {
                 logp_grad_tiny_kernel<T, mask.value><<<(unsigned)up(a.rows, kTinyThreads), kTinyThreads, 0, st>>>(
                     a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride);
+            } else if (a.V <= kGradWarp) {
+                logp_wide_grad_kernel<T, 32, mask.value>
+                    <<<(unsigned)up(a.rows, kGradThreads / 32), kGradThreads, 0, st>>>(
+                        a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride, packed);
             } else {
                 const int parts = (int)up(a.V, 16384);  // (of a row; blocks of some 16,384 entries)
-                logp_wide_grad_kernel<T, mask.value>
+                logp_wide_grad_kernel<T, kGradThreads, mask.value>
                     <<<dim3((unsigned)a.rows, (unsigned)(parts < 65535 ? parts : 65535)), kGradThreads, 0, st>>>(
                         a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride, packed);
             }

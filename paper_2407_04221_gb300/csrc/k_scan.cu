@@ -10,9 +10,10 @@
 // and go by TMA through shared memory, the next one under way during this one,
 // results leaving from the places of the inputs they came from.  The tensor
 // maps lay step k of all eight runs side by side, so that the 128-byte swizzle
-// sends lanes of different runs to different banks.  (Chunks that reach past
-// the sequence, and arrays that TMA does not take, go by cp.async or by single
-// values, to the same places.)  Both directions read and write their arrays
+// sends lanes of different runs to different banks.  (A chunk that reaches past
+// the sequence goes by cp.async, to the same places.)  Arrays that TMA does not
+// take, of odd widths or strides, come row by row by bulk copies of the 16-byte
+// pieces that hold a row's values.  Both directions read and write their arrays
 // once: 3 and 5 values a step and channel.  The backward pass makes the states
 // again from the one kept at each chunk's start (4 bytes a chunk and channel),
 // so it neither reads h nor suffers its rounding.  Bound by memory, and for
@@ -22,7 +23,7 @@
 // fill the GPU, a sequence is cut into segments: a first pass makes every
 // segment's map, a second walks the segments from the states that the maps
 // before them give, in one order.  The inputs are read twice then, but no block
-// waits for another.  Up to 16 steps of many channels take a thread each for
+// waits for another.  Up to eight steps (16 of 32 bits) of many channels take a thread each for
 // two channels.
 //
 // A step that begins an episode forgets the state even where it is NaN: in a
@@ -146,7 +147,7 @@ struct Args {
     uint32_t segments, per;     // segments of a sequence, chunks of a segment
     Map2 *maps;                 // [slab][segment][kMaps], where there are several segments
     bool flat;                  // sequences lie side by side: channels are numbered through
-    int in_bytes, out_bytes;    // of a copy: 16, 4, or 0 where values are copied one by one
+    int words[2];               // of the outputs: whether 32-bit words of them can be stored
 };
 // The arrays for TMA: inputs, outputs.
 struct TensorMaps {
@@ -235,58 +236,125 @@ __device__ __forceinline__ int place_of(int step, int channel)
 template <class T>
 __device__ constexpr int step_of() { return kRuns * 128 / (int)sizeof(T); }
 
-// Calls f(pointer, place) for all of a chunk's pieces of kPer channels that are
-// there, dealt to the block's threads; p: the array's first value of the chunk.
-template <class T, int kRun, int kPer, class P, class F>
+// f(pointer, place) for the 16-byte pieces of a chunk that are there, dealt to
+// the block's threads; p: the array's first value of the chunk.
+template <class T, int kRun, class P, class F>
 __device__ __forceinline__ void pieces(P *p, int64_t stride, int steps, int width, F f)
 {
-    constexpr int kAcross = kSlab / kPer, kDown = kThreads / kAcross;
+    constexpr int kPer = 16 / sizeof(T), kAcross = kSlab / kPer, kDown = kThreads / kAcross;
     const int channel = threadIdx.x % kAcross * kPer, first = threadIdx.x / kAcross;
     if (channel >= width)
         return;
     p += first * stride + channel;
-#pragma unroll 4
+#pragma unroll 2
     for (int k = first; k < steps; k += kDown, p += kDown * stride)
         f(p, place_of<T, kRun>(k, channel));
 }
 
 // A chunk of an array to shared memory, as far as there are steps and channels.
 template <class T, int kRun>
-__device__ __noinline__ void bring(T *to, const void *from, int64_t st, int64_t sb, const Item &s, int64_t t0,
-                                   int steps, int bytes)
+__device__ __noinline__ void bring(T *to, const void *from, int64_t st, int64_t sb, const Item &s, int64_t t0, int steps)
 {
-    const T *p = (const T *)from + t0 * st + s.b * sb + s.d;
     const uint32_t dst = smem_addr(to);
-    if (bytes == 16)
-        pieces<T, kRun, 16 / sizeof(T)>(p, st, steps, s.width, [&](const T *q, int at) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(at * sizeof(T))), "l"(q)
-                         : "memory");
-        });
-    else if (bytes == 4)
-        pieces<T, kRun, 4 / sizeof(T)>(p, st, steps, s.width, [&](const T *q, int at) {
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (uint32_t)(at * sizeof(T))), "l"(q)
-                         : "memory");
-        });
-    else
-        pieces<T, kRun, 1>(p, st, steps, s.width, [&](const T *q, int at) { to[at] = *q; });
+    pieces<T, kRun>((const T *)from + t0 * st + s.b * sb + s.d, st, steps, s.width, [&](const T *q, int at) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(at * sizeof(T))), "l"(q)
+                     : "memory");
+    });
 }
 
 // And back.
 template <class T, int kRun>
 __device__ __noinline__ void take_out(const T *from, void *to, int64_t st, int64_t sb, const Item &s, int64_t t0,
-                                      int steps, int bytes)
+                                      int steps)
 {
-    T *p = (T *)to + t0 * st + s.b * sb + s.d;
-    if (bytes == 16)
-        pieces<T, kRun, 16 / sizeof(T)>(p, st, steps, s.width, [&](T *q, int at) {
-            *reinterpret_cast<uint4 *>(q) = *reinterpret_cast<const uint4 *>(from + at);
-        });
-    else if (bytes == 4)
-        pieces<T, kRun, 4 / sizeof(T)>(p, st, steps, s.width, [&](T *q, int at) {
-            *reinterpret_cast<uint32_t *>(q) = *reinterpret_cast<const uint32_t *>(from + at);
-        });
-    else
-        pieces<T, kRun, 1>(p, st, steps, s.width, [&](T *q, int at) { *q = from[at]; });
+    pieces<T, kRun>((T *)to + t0 * st + s.b * sb + s.d, st, steps, s.width, [&](T *q, int at) {
+        *reinterpret_cast<uint4 *>(q) = *reinterpret_cast<const uint4 *>(from + at);
+    });
+}
+
+// Rows by bulk copies: bytes from one row to the next, an odd number of 16-byte
+// pieces, so that runs' rows, side by side, are in different banks.
+template <class T>
+__host__ __device__ constexpr int pitch_of() { return kSlab * (int)sizeof(T) + 16; }
+template <class T, int kRun>
+__host__ __device__ constexpr int rows_bytes() { return kRun * kRuns * pitch_of<T>(); }
+// The row of a step.
+template <int kRun>
+__device__ __forceinline__ int row_of(int step) { return step % kRun * kRuns + step / kRun; }
+
+// This thread's rows of a chunk's arrays to shared memory; it arrives at the
+// barrier with their bytes.
+template <class T, int kRun, int kArrays>
+__device__ __forceinline__ void bring_rows(uint32_t to, const Args &a, const int (&array)[kArrays], const Item &s,
+                                           int64_t t0, int steps, uint32_t bar)
+{
+    constexpr int kChunk = kRun * kRuns, kTurns = (kArrays * kChunk + kThreads - 1) / kThreads;
+    const char *from[kTurns];
+    uint32_t bytes[kTurns], all = 0;
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+        const int row = threadIdx.x + j * kThreads, k = row / kChunk, t = row % kChunk;
+        bytes[j] = 0;
+        if (k < kArrays && t < steps) {
+            const void *p = a.in[array[0]];
+            int64_t st = a.it[array[0]], sb = a.ib[array[0]];
+#pragma unroll
+            for (int q = 1; q < kArrays; ++q)
+                if (k == q) {
+                    p = a.in[array[q]];
+                    st = a.it[array[q]];
+                    sb = a.ib[array[q]];
+                }
+            const T *first = (const T *)p + (t0 + t) * st + s.b * sb + s.d;
+            const uint32_t lead = (uint32_t)reinterpret_cast<uintptr_t>(first) & 15;
+            from[j] = reinterpret_cast<const char *>(first) - lead;
+            bytes[j] = (lead + s.width * (uint32_t)sizeof(T) + 15) & ~15u;
+            all += bytes[j];
+        }
+    }
+    bar_expect(bar, all);
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+        const int row = threadIdx.x + j * kThreads;
+        if (bytes[j])
+            bulk_load(to + (row / kChunk) * rows_bytes<T, kRun>() + row_of<kRun>(row % kChunk) * pitch_of<T>(), from[j],
+                      bytes[j], bar);
+    }
+}
+
+// The bytes before a row's first value, of step t from the chunk's start.
+template <class T>
+__device__ __forceinline__ uint32_t lead_of(const void *p, int64_t st, int64_t sb, const Item &s, int64_t t)
+{
+    return (uint32_t)reinterpret_cast<uintptr_t>((const T *)p + t * st + s.b * sb + s.d) & 15;
+}
+
+// Results, in the places of array k's rows (whose leads they have), out.
+template <class T, int kRun>
+__device__ __noinline__ void rows_out(const char *from, const Args &a, int k, const Item &s, int64_t t0, int steps)
+{
+    const char *rows = from + k * rows_bytes<T, kRun>();
+    T *p = (T *)a.out[k] + t0 * a.ot[k] + s.b * a.ob[k] + s.d;
+    const uint32_t lead0 = lead_of<T>(a.in[k], a.it[k], a.ib[k], s, t0), step = (uint32_t)(a.it[k] * sizeof(T)) & 15;
+    if (sizeof(T) == 2 && a.words[k]) {  // a word of two values a lane, a row a warp
+        const int c = (threadIdx.x & 31) * 2;
+#pragma unroll 4
+        for (int t = threadIdx.x >> 5; t < steps; t += kWarps) {
+            const T *q = reinterpret_cast<const T *>(rows + row_of<kRun>(t) * pitch_of<T>() + ((lead0 + t * step) & 15)) + c;
+            const T v[2] = {q[0], q[1]};
+            if (c + 1 < s.width)
+                *reinterpret_cast<uint32_t *>(p + t * a.ot[k] + c) = *reinterpret_cast<const uint32_t *>(v);
+            else if (c < s.width)
+                p[t * a.ot[k] + c] = v[0];
+        }
+        return;
+    }
+    const int c = threadIdx.x % kSlab;
+#pragma unroll 4
+    for (int t = threadIdx.x / kSlab; t < steps; t += kThreads / kSlab)
+        if (c < s.width)
+            p[t * a.ot[k] + c] =
+                reinterpret_cast<const T *>(rows + row_of<kRun>(t) * pitch_of<T>() + ((lead0 + t * step) & 15))[c];
 }
 
 // Steps past the sequence's end change nothing: gates of 1, values and
@@ -328,6 +396,18 @@ __device__ __forceinline__ float2 marked_by(float2 v, uint32_t bits, int k)
     v.x = __uint_as_float(__float_as_uint(v.x) ^ (bits << (31 - k) & 0x80000000u));
     v.y = __uint_as_float(__float_as_uint(v.y) ^ (bits << (15 - k) & 0x80000000u));
     return v;
+}
+
+// The same for rows, whatever their leads.
+template <class T, int kRun>
+__device__ __noinline__ void pad_rows(char *tile, int steps, int arrays)
+{
+    constexpr int kPer = pitch_of<T>() / (int)sizeof(T);
+    for (int k = steps * kPer + threadIdx.x; k < kRun * kRuns * kPer; k += kThreads) {
+        const int at = row_of<kRun>(k / kPer) * kPer + k % kPer;
+        for (int array = 0; array < arrays; ++array)
+            reinterpret_cast<T *>(tile + array * rows_bytes<T, kRun>())[at] = from_f32<T>(array == 0 ? INFINITY : 0.0f);
+    }
 }
 
 // Bits k (first channel) and 16 + k (second) for the steps of this lane's run
@@ -378,6 +458,29 @@ struct Tile {
     __device__ __forceinline__ void put(int array, int k, float2 v) const
     {
         write2(p + array * (kRun * kRuns * kSlab) + k * step_of<T>(), v);
+    }
+};
+
+// The same where rows came by bulk copies: each has its lead.
+template <class T, int kRun, int kArrays>
+struct Rows {
+    char *p;  // the run's first row and the lane's channel, without a lead
+    uint32_t lead[kArrays], step[kArrays];
+    __device__ __forceinline__ T *at(int array, int k) const
+    {
+        return reinterpret_cast<T *>(p + array * rows_bytes<T, kRun>() + k * kRuns * pitch_of<T>() +
+                                     ((lead[array] + k * step[array]) & 15));
+    }
+    __device__ __forceinline__ float2 get(int array, int k) const
+    {
+        const T *q = at(array, k);
+        return make_float2(to_f32(q[0]), to_f32(q[1]));
+    }
+    __device__ __forceinline__ void put(int array, int k, float2 v) const
+    {
+        T *q = at(array, k);
+        q[0] = from_f32<T>(v.x);
+        q[1] = from_f32<T>(v.y);
     }
 };
 
@@ -585,9 +688,18 @@ __host__ __device__ constexpr int blocks_of(int e, bool back, int run)
 {
     return run == kLongRun ? 2 : run == 4 || e == 2 ? 4 : back ? 2 : 3;
 }
-// Chunks in shared memory: the one that is taken and the next; forward also
-// one whose results are leaving.
-__host__ __device__ constexpr int stages_of(bool back, bool maps_only) { return back || maps_only ? 2 : 3; }
+// Chunks in shared memory: the one that is taken and the next; forward by TMA
+// also one whose results are leaving.
+__host__ __device__ constexpr int stages_of(bool back, bool maps_only, bool tma)
+{
+    return back || maps_only || !tma ? 2 : 3;
+}
+// Bytes of an array's chunk.
+template <class T, int kRun>
+__host__ __device__ constexpr int chunk_bytes(bool tma)
+{
+    return tma ? kRun * kRuns * kSlab * (int)sizeof(T) : rows_bytes<T, kRun>();
+}
 
 // kBack: chunks from the last to the first.  What flows to before step t is
 // m_t = a_t k_t l_t, l_t = dh_t + m_{t+1}: a run's map of it has the forward
@@ -599,61 +711,66 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
     const __grid_constant__ TensorMaps tma, const Args a)
 {
     constexpr int kArrays = kBack && !kMapsOnly ? 3 : 2, kOut = kMapsOnly ? 0 : kBack ? 2 : 1;
-    constexpr int kChunk = kRun * kRuns, kTile = kChunk * kSlab, kStages = stages_of(kBack, kMapsOnly);
-    constexpr int kBoxes = sizeof(T) / 2, kBox = kTile / kBoxes;  // of an array's chunk; values of one
+    constexpr int kChunk = kRun * kRuns, kStages = stages_of(kBack, kMapsOnly, kTma);
+    constexpr int kBytes = chunk_bytes<T, kRun>(kTma);            // of an array's chunk
+    constexpr int kBoxes = sizeof(T) / 2, kBox = kBytes / kBoxes;  // of it by TMA; bytes of one
     extern __shared__ uint8_t raw[];
     __shared__ Item items[4];
     __shared__ uint64_t bars[kStages];
     __shared__ int dead;
-    T *tiles = reinterpret_cast<T *>(raw + ((1024 - (smem_addr(raw) & 1023)) & 1023));
-    const int channel = (threadIdx.x >> 5) * 8 + 2 * (threadIdx.x & 3);
-    const int spot = place_of<T, kRun>((threadIdx.x & 31) / 4 * kRun, channel);  // of the run's first step
-    auto stage = [&](int s) { return tiles + s * kArrays * kTile; };
-    // which of the call's arrays the k-th of the tile is
-    auto array_of = [](int k) { return kBack && kMapsOnly && k == 1 ? 2 : k; };
-    auto by_tma = [&](const Item &t) {
-        const int64_t t0 = (int64_t)(kBack ? a.chunks - 1 - t.place : t.place) * kChunk;
-        return kTma && a.T - t0 >= kChunk;
-    };
+    char *tiles = reinterpret_cast<char *>(raw + ((1024 - (smem_addr(raw) & 1023)) & 1023));
+    const int channel = (threadIdx.x >> 5) * 8 + 2 * (threadIdx.x & 3), run_at = (threadIdx.x & 31) / 4 * kRun;
+    auto stage = [&](int s, int k = 0) { return tiles + (s * kArrays + k) * kBytes; };
+    // which of the call's arrays are the tile's
+    const int arrays[3] = {0, kBack && kMapsOnly ? 2 : 1, 2};
+    auto time_of = [&](const Item &t) { return (int64_t)(kBack ? a.chunks - 1 - t.place : t.place) * kChunk; };
+    auto steps_at = [&](int64_t t0) { return (int)(a.T - t0 < kChunk ? a.T - t0 : kChunk); };
+    auto by_tma = [&](const Item &t) { return kTma && a.T - time_of(t) >= kChunk; };
     // all threads: an item's chunk to stage s
     auto fill = [&](const Item &t, int s) {
         if (t.width > 0) {
-            const int64_t t0 = (int64_t)(kBack ? a.chunks - 1 - t.place : t.place) * kChunk;
-            if (by_tma(t)) {
+            const int64_t t0 = time_of(t);
+            const uint32_t bar = smem_addr(bars + s);
+            if constexpr (!kTma) {
+                int which[kArrays];
+#pragma unroll
+                for (int k = 0; k < kArrays; ++k)
+                    which[k] = arrays[k];
+                bring_rows<T, kRun, kArrays>(smem_addr(stage(s)), a, which, t, t0, steps_at(t0), bar);
+            } else if (by_tma(t)) {
                 if (threadIdx.x == 0) {
                     // (what left from this stage has been read)
                     if constexpr (kOut > 0)
                         asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kStages - 2) : "memory");
-                    const uint32_t bar = smem_addr(bars + s);
-                    bar_expect(bar, kArrays * kTile * sizeof(T));
+                    bar_expect(bar, kArrays * kBytes);
 #pragma unroll
                     for (int k = 0; k < kArrays; ++k)
 #pragma unroll
                         for (int q = 0; q < kBoxes; ++q)
-                            tma_load(smem_addr(stage(s) + k * kTile + q * kBox), &tma.in[array_of(k)],
+                            tma_load(smem_addr(stage(s, k)) + q * kBox, &tma.in[arrays[k]],
                                      (int)t.d + q * (kSlab / kBoxes), (int)(t0 / kRun), (int)t.b, bar);
                 }
             } else {
-                if (kTma && kOut > 0) {
+                if (kOut > 0) {
                     if (threadIdx.x == 0)
                         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncthreads();
                 }
-                const int steps = (int)(a.T - t0 < kChunk ? a.T - t0 : kChunk);
 #pragma unroll
                 for (int k = 0; k < kArrays; ++k) {
-                    const int q = array_of(k);
-                    bring<T, kRun>(stage(s) + k * kTile, a.in[q], a.it[q], a.ib[q], t, t0, steps, a.in_bytes);
+                    const int q = arrays[k];
+                    bring<T, kRun>(reinterpret_cast<T *>(stage(s, k)), a.in[q], a.it[q], a.ib[q], t, t0, steps_at(t0));
                 }
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (kTma)
+            asm volatile("cp.async.commit_group;" ::: "memory");
     };
     Order order{blockIdx.x, 0, 0};  // thread 0's
     if (threadIdx.x == 0) {
         dead = 0;
         for (int s = 0; s < kStages; ++s)
-            bar_init(smem_addr(bars + s), 1);
+            bar_init(smem_addr(bars + s), kTma ? 1 : kThreads);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         order.open(a);
         order.next(a, items[0]);
@@ -667,11 +784,13 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
     float carry[2] = {};       // the state that enters the next chunk, in every run's lanes
     int s = 0;
     for (uint32_t i = 0; items[i & 3].width > 0; ++i) {
-        if (by_tma(items[i & 3])) {
+        if (!kTma || by_tma(items[i & 3])) {
             ok = ok && bar_wait(smem_addr(bars + s), phases >> s & 1, &dead);
             phases ^= 1u << s;
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (kTma)
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (before copies to where this thread read or wrote)
         __syncthreads();  // this chunk is here, the one before is done with
         const int s_next = s + 1 == kStages ? 0 : s + 1;
         fill(items[(i + 1) & 3], s_next);
@@ -680,10 +799,27 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
         const Item item = items[i & 3];
         const Chunk c = chunk_of<kBack, kChunk>(a, item, channel);
         if (c.steps < kChunk) {
-            pad<T, kRun>(stage(s), c.steps, kArrays);
+            if (kTma)
+                pad<T, kRun>(reinterpret_cast<T *>(stage(s)), c.steps, kArrays);
+            else
+                pad_rows<T, kRun>(stage(s), c.steps, kArrays);
             __syncthreads();
         }
-        const Tile<T, kRun> tile{stage(s) + spot};
+        const auto tile = [&] {
+            if constexpr (kTma) {
+                return Tile<T, kRun>{reinterpret_cast<T *>(stage(s)) + place_of<T, kRun>(run_at, channel)};
+            } else {
+                Rows<T, kRun, kArrays> rows;
+                rows.p = stage(s) + (run_at / kRun) * pitch_of<T>() + channel * sizeof(T);
+#pragma unroll
+                for (int k = 0; k < kArrays; ++k) {
+                    const int q = arrays[k];
+                    rows.lead[k] = lead_of<T>(a.in[q], a.it[q], a.ib[q], item, c.t0 + run_at);
+                    rows.step[k] = (uint32_t)(a.it[q] * sizeof(T)) & 15;
+                }
+                return rows;
+            }
+        }();
         Run<kBack, kRun> run;
         run.resets = resets_of<kRun>(a, item, c.t0, c.steps);
         run.plain = __all_sync(~0u, run.resets == 0);
@@ -756,21 +892,26 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
 #pragma unroll
                         for (int q = 0; q < kBoxes; ++q)
                             if (q * (kSlab / kBoxes) < item.width)
-                                tma_store(&tma.out[k], smem_addr(stage(s) + k * kTile + q * kBox),
+                                tma_store(&tma.out[k], smem_addr(stage(s, k)) + q * kBox,
                                           (int)item.d + q * (kSlab / kBoxes), (int)(c.t0 / kRun), (int)item.b);
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < kOut; ++k)
-                    take_out<T, kRun>(stage(s) + k * kTile, a.out[k], a.ot[k], a.ob[k], items[i & 3], c.t0, c.steps,
-                                      a.out_bytes);
+                for (int k = 0; k < kOut; ++k) {
+                    if constexpr (kTma)
+                        take_out<T, kRun>(reinterpret_cast<const T *>(stage(s, k)), a.out[k], a.ot[k], a.ob[k],
+                                          items[i & 3], c.t0, c.steps);
+                    else
+                        rows_out<T, kRun>(stage(s), a, k, items[i & 3], c.t0, c.steps);
+                }
             }
             if (kTma && threadIdx.x == 0)
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
         s = s_next;
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (kTma)
+        asm volatile("cp.async.wait_all;" ::: "memory");
     if (kTma && kOut > 0 && threadIdx.x == 0)
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     if (!ok)
@@ -982,17 +1123,6 @@ int64_t work_bytes(int64_t T, int64_t B, int64_t D, int e)
     return most;
 }
 
-// How an array's values can be copied, given those before it: 16 or 4 bytes at
-// once, or one by one (0).  A copy reads no further than the array's own row.
-int copy_bytes(int so_far, const void *p, int64_t t, int64_t b, int64_t n, int e)
-{
-    auto fits = [&](int bytes) {
-        return so_far >= bytes && (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 && t * e % bytes == 0 &&
-               b * e % bytes == 0 && n * e % bytes == 0;
-    };
-    return fits(16) ? 16 : fits(4) ? 4 : 0;
-}
-
 // An array for TMA: channels, runs, a run's steps, sequences.
 bool array_map(CUtensorMap *map, int dtype, const void *p, int64_t n, int64_t T, int run, int64_t st, int64_t B, int64_t sb)
 {
@@ -1015,21 +1145,27 @@ cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
     a.per = (uint32_t)up(chunks, segments);
     a.maps = (Map2 *)work;
     const int64_t n = a.flat ? a.B * a.D : a.D, sequences = a.flat ? 1 : a.B;
-    a.in_bytes = a.out_bytes = 16;
-    for (int k = 0; k < kArrays; ++k)
-        a.in_bytes = copy_bytes(a.in_bytes, a.in[k], a.it[k], a.flat ? 0 : a.ib[k], n, sizeof(T));
-    for (int k = 0; k < kOut; ++k)
-        a.out_bytes = copy_bytes(a.out_bytes, a.out[k], a.ot[k], a.flat ? 0 : a.ob[k], n, sizeof(T));
-    TensorMaps maps;
-    bool tma = a.in_bytes == 16 && a.out_bytes == 16 && a.T >= kRun * kRuns && n < (int64_t(1) << 31) &&
+    // rows of whole 16-byte pieces, a whole chunk of them at least
+    bool tma = n * (int64_t)sizeof(T) % 16 == 0 && a.T >= kRun * kRuns && n < (int64_t(1) << 31) &&
                sequences < (int64_t(1) << 31);
+    auto whole_pieces = [&](const void *p, int64_t t, int64_t b) {
+        tma = tma && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && t * (int64_t)sizeof(T) % 16 == 0 &&
+              (a.flat || b * (int64_t)sizeof(T) % 16 == 0);
+    };
+    for (int k = 0; k < kArrays; ++k)
+        whole_pieces(a.in[k], a.it[k], a.ib[k]);
+    for (int k = 0; k < kOut; ++k) {
+        whole_pieces(a.out[k], a.ot[k], a.ob[k]);
+        a.words[k] = (reinterpret_cast<uintptr_t>(a.out[k]) & 3) == 0 && a.ot[k] % 2 == 0 && (a.flat || a.ob[k] % 2 == 0);
+    }
+    TensorMaps maps{};
     for (int k = 0; k < kArrays && tma; ++k)
         tma = array_map(&maps.in[k], dtype, a.in[k], n, a.T, kRun, a.it[k], sequences, a.ib[k]);
     for (int k = 0; k < kOut && tma; ++k)
         tma = array_map(&maps.out[k], dtype, a.out[k], n, a.T, kRun, a.ot[k], sequences, a.ob[k]);
     const int64_t units = slabs * segments, grid = units < resident ? units : resident;
     auto run = [&](auto kernel, int stages, int arrays) {
-        const int bytes = stages * arrays * kRun * kRuns * kSlab * (int)sizeof(T) + 1024;
+        const int bytes = stages * arrays * chunk_bytes<T, kRun>(tma) + 1024;
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess)
             return e;
@@ -1037,13 +1173,13 @@ cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
         return cudaGetLastError();
     };
     if (segments > 1) {
-        const int stages = stages_of(kBack, true);
+        const int stages = stages_of(kBack, true, tma);
         const cudaError_t e = tma ? run(walk_kernel<T, kBack, true, true, kRun>, stages, 2)
                                   : run(walk_kernel<T, kBack, true, false, kRun>, stages, 2);
         if (e != cudaSuccess)
             return e;
     }
-    const int stages = stages_of(kBack, false);
+    const int stages = stages_of(kBack, false, tma);
     return tma ? run(walk_kernel<T, kBack, false, true, kRun>, stages, kArrays)
                : run(walk_kernel<T, kBack, false, false, kRun>, stages, kArrays);
 }
@@ -1074,8 +1210,14 @@ cudaError_t launch(Args &a, int dtype, void *work, cudaStream_t st)
         a.flat = a.flat && (a.B == 1 || a.ob[k] == a.D);
     return with_type(dtype, [&](auto v) {
         using T = decltype(v);
-        if (a.T <= 16 && a.B * a.D >= kBriefChannels)
-            return a.T <= 4 ? brief<T, kBack, 4>(a, st) : a.T <= 8 ? brief<T, kBack, 8>(a, st) : brief<T, kBack, 16>(a, st);
+        if (a.B * a.D >= kBriefChannels) {
+            if (a.T <= 8)
+                return a.T <= 4 ? brief<T, kBack, 4>(a, st) : brief<T, kBack, 8>(a, st);
+            if constexpr (sizeof(T) == 4) {  // (16 steps of 16-bit values: 125 us against 107 walked, of 32-bit ones 50 against 114)
+                if (a.T <= 16)
+                    return brief<T, kBack, 16>(a, st);
+            }
+        }
         const int run = run_of(a.T, sizeof(T));
         if constexpr (sizeof(T) == 2) {
             if (run == kLongRun)
