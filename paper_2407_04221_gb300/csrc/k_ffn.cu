@@ -13,8 +13,10 @@
 // pass makes g and u again (4 M D H operations of 16) instead of keeping them:
 // kept in 16 bits they would cost accuracy, in 32 bits 8 bytes a unit.
 //
-// Warps: one issues copies (TMA), one products, four take accumulators to
-// memory while the next tile's products run (two sets of 256 TMEM columns).
+// Warps: one issues copies (TMA), one products, four or eight take accumulators
+// to memory while the next tile's products run (two sets of 256 TMEM columns).
+// The gated forms take eight: with four the backward one spent more time on
+// activations than on products (16,384 x 1,024 x 4,096: 204 us).
 #include "async.cuh"
 #include "policy.h"
 #include "tensor_map.h"
@@ -40,7 +42,7 @@ __device__ __forceinline__ void activate(float g, float &f, float &slope)
 
 // ------------------------------------------------------------ few rows
 
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 4;  // (eight: 18.6 us, 16: 28.8, by tensor cores 12.5, at 1,024 x 4,096)
 constexpr int kFewThreads = 256;
 
 template <class T>
@@ -110,10 +112,7 @@ constexpr int kRowsCta = 128;  // accumulator rows of a CTA, and B rows it fetch
 constexpr int kTile = 256;     // rows and columns of a pair's tile
 constexpr int kBlockK = 64;    // terms a stage: 128 bytes, the swizzle's width
 constexpr int kHalf = kRowsCta * kBlockK * 2;  // bytes of A or of B a CTA fetches per stage
-constexpr int kStages = 6;
 constexpr int kSlab = kRowsCta * 128;  // staging of 128 rows x 128 bytes on the way out
-constexpr int kSmem = kStages * 2 * kHalf + 2 * kSlab + 1024 + 256;
-constexpr int kThreads = 192;
 constexpr int kTmemCols = 512;
 
 enum Form {
@@ -122,6 +121,16 @@ enum Form {
     kTimesW,   // dx = dgu w: B runs along its rows
     kTransposed // dw = dgu^T x: A and B run along their rows
 };
+
+// Fours of warps that take accumulators out; slabs of each; stages of A and B.
+__host__ __device__ constexpr int teams_of(int form) { return form == kForward || form == kProjGrad ? 2 : 1; }
+__host__ __device__ constexpr int slabs_of(int form) { return form == kForward ? 1 : 2; }
+__host__ __device__ constexpr int stages_of(int form) { return form == kProjGrad ? 5 : 6; }
+__host__ __device__ constexpr int threads_of(int form) { return 64 + 128 * teams_of(form); }
+__host__ __device__ constexpr int smem_of(int form)
+{
+    return stages_of(form) * 2 * kHalf + teams_of(form) * slabs_of(form) * kSlab + 1024 + 256;
+}
 
 struct Params {
     int m, n;               // rows and columns of the result (forward forms: columns of H)
@@ -248,10 +257,10 @@ __device__ __forceinline__ void put32(uint32_t slab, int row, int half, const fl
               pack2<T>(v[8 * c + 4], v[8 * c + 5]), pack2<T>(v[8 * c + 6], v[8 * c + 7]));
 }
 
-__device__ __forceinline__ void epilogue_sync()
+__device__ __forceinline__ void team_sync(int team)
 {
     __syncwarp();
-    asm volatile("bar.sync 1, 128;" ::: "memory");
+    asm volatile("bar.sync %0, 128;" ::"r"(team + 1) : "memory");
 }
 
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -279,16 +288,17 @@ __device__ __forceinline__ Tile tile_of(const Params &p, int i)
 }
 
 template <class T, int kForm, int kAct, bool kParts>
-__global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_kernel(
+__global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) void ffn_kernel(
     const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
     const __grid_constant__ CUtensorMap out_map, const Params p)
 {
     constexpr bool kARows = kForm == kTransposed, kBRows = kForm == kTimesW || kForm == kTransposed;
     constexpr bool kGated = kForm == kForward || kForm == kProjGrad;
+    constexpr int kTeams = teams_of(kForm), kSlabs = slabs_of(kForm), kStages = stages_of(kForm);
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t slabs = base + kStages * 2 * kHalf;
-    const uint32_t bars = slabs + 2 * kSlab;
+    const uint32_t bars = slabs + kTeams * kSlabs * kSlab;
     // barriers: full[stage], empty[stage], acc_full[2], acc_empty[2]
     const uint32_t full = bars, empty = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 16;
     uint8_t *tail = raw + (bars + 16 * kStages + 32 - smem_addr(raw));
@@ -308,7 +318,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(acc_full + 8 * s, 1);
-            bar_init(acc_empty + 8 * s, 8);  // four warps in either CTA
+            bar_init(acc_empty + 8 * s, 8 * kTeams);  // the teams' warps in either CTA
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -388,7 +398,9 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
         }
     } else {
         const int quarter = warp & 3, row = quarter * 32 + lane;
-        const bool first = threadIdx.x == 64;
+        const int team = (warp - 2) >> 2;
+        const bool first = (threadIdx.x - 64) % 128 == 0;  // issues its team's stores
+        const uint32_t slab0 = slabs + team * kSlabs * kSlab;
         int done = 0;
         for (int i = pair; i < tiles; i += pairs, ++done) {
             const Tile t = tile_of(p, i);
@@ -409,15 +421,11 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
             };
             if (kGated) {
 #pragma unroll 1
-                for (int c = 0; c < kRowsCta; c += 64) {  // 64 columns of H
-                    if (first) {
-                        if (kForm == kForward)
-                            stores_left<1>();
-                        else
-                            stores_left<0>();
-                    }
-                    epilogue_sync();
-                    const uint32_t slab = slabs + (kForm == kForward ? (c >> 6) * kSlab : 0);
+                for (int c = team * 64; c < kRowsCta; c += 64 * kTeams) {  // 64 columns of H a team
+                    if (first)
+                        stores_left<0>();
+                    team_sync(team);
+                    const uint32_t slab = slab0;
 #pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
                         float g[32], u[32];
@@ -456,7 +464,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
                         }
                     }
                     fence_async();
-                    epilogue_sync();
+                    team_sync(team);
                     if (first && t.n * kRowsCta + c < p.n && m0 < p.m) {
                         const int col = t.n * kRowsCta + c;
                         store_box(&out_map, slab, col, 0, m0);
@@ -472,8 +480,8 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
                 for (int c = 0; c < kTile; c += kWide) {
                     if (first)
                         stores_left<1>();
-                    epilogue_sync();
-                    const uint32_t slab = slabs + (c / kWide & 1) * kSlab;
+                    team_sync(team);
+                    const uint32_t slab = slab0 + (c / kWide & 1) * kSlab;
                     float v[32];
                     if (kParts) {
                         columns(c, v);
@@ -491,7 +499,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) void ffn_ker
                         }
                     }
                     fence_async();
-                    epilogue_sync();
+                    team_sync(team);
                     if (first && t.n * kTile + c < p.n && m0 < p.m)
                         store_box(&out_map, slab, t.n * kTile + c, m0, t.split);
                     if (first)
@@ -580,11 +588,11 @@ template <class T, int kForm, int kAct, bool kParts>
 cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Params &p, cudaStream_t st)
 {
     const auto kernel = ffn_kernel<T, kForm, kAct, kParts>;  // (kAct plays no part in the last two forms)
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kForm));
     if (e != cudaSuccess)
         return e;
     const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles * p.splits;
-    kernel<<<2 * (unsigned)(tiles < kPairs ? tiles : kPairs), kThreads, kSmem, st>>>(a, b, out, p);
+    kernel<<<2 * (unsigned)(tiles < kPairs ? tiles : kPairs), threads_of(kForm), smem_of(kForm), st>>>(a, b, out, p);
     return cudaGetLastError();
 }
 
@@ -629,8 +637,6 @@ void few(int rows, int64_t D, int64_t H, const T *x, int64_t xs, const T *w, T *
     const unsigned grid = (unsigned)up(H, kFewThreads / 32);
     if (rows <= 1)
         ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
-    else if (rows <= 4)
-        ffn_few_kernel<T, kAct, 4, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
     else
         ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
 }

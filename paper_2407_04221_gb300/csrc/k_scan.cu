@@ -461,8 +461,9 @@ struct Tile {
     }
 };
 
-// The same where rows came by bulk copies: each has its lead.
-template <class T, int kRun, int kArrays>
+// The same where rows came by bulk copies: each has its lead.  kPairs: of whole
+// 32-bit words, so that two 16-bit values are one.
+template <class T, int kRun, int kArrays, bool kPairs>
 struct Rows {
     char *p;  // the run's first row and the lane's channel, without a lead
     uint32_t lead[kArrays], step[kArrays];
@@ -474,13 +475,19 @@ struct Rows {
     __device__ __forceinline__ float2 get(int array, int k) const
     {
         const T *q = at(array, k);
+        if constexpr (kPairs)
+            return read2(q);
         return make_float2(to_f32(q[0]), to_f32(q[1]));
     }
     __device__ __forceinline__ void put(int array, int k, float2 v) const
     {
         T *q = at(array, k);
-        q[0] = from_f32<T>(v.x);
-        q[1] = from_f32<T>(v.y);
+        if constexpr (kPairs) {
+            write2(q, v);
+        } else {
+            q[0] = from_f32<T>(v.x);
+            q[1] = from_f32<T>(v.y);
+        }
     }
 };
 
@@ -686,13 +693,13 @@ __device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, 
 // Blocks of an SM: as many as registers and shared memory hold.
 __host__ __device__ constexpr int blocks_of(int e, bool back, int run)
 {
-    return run == kLongRun ? 2 : run == 4 || e == 2 ? 4 : back ? 2 : 3;
+    return run == kLongRun ? 2 : run == 4 ? 4 : back ? 2 : 3;
 }
 // Chunks in shared memory: the one that is taken and the next; forward by TMA
 // also one whose results are leaving.
-__host__ __device__ constexpr int stages_of(bool back, bool maps_only, bool tma)
+__host__ __device__ constexpr int stages_of(int e, bool back, bool maps_only, bool tma)
 {
-    return back || maps_only || !tma ? 2 : 3;
+    return e == 4 || back || maps_only || !tma ? 2 : 3;
 }
 // Bytes of an array's chunk.
 template <class T, int kRun>
@@ -701,17 +708,21 @@ __host__ __device__ constexpr int chunk_bytes(bool tma)
     return tma ? kRun * kRuns * kSlab * (int)sizeof(T) : rows_bytes<T, kRun>();
 }
 
+// How chunks come: by TMA, or row by row, of pairs of 16-bit values or singly.
+enum Way { kByTma, kByPairs, kBySingles };
+
 // kBack: chunks from the last to the first.  What flows to before step t is
 // m_t = a_t k_t l_t, l_t = dh_t + m_{t+1}: a run's map of it has the forward
 // map's factor.
 // kMapsOnly: no outputs but the segments' maps (backward these take gates and
 // dh alone).
-template <class T, bool kBack, bool kMapsOnly, bool kTma, int kRun>
+template <class T, bool kBack, bool kMapsOnly, int kWay, int kRun>
 __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void walk_kernel(
     const __grid_constant__ TensorMaps tma, const Args a)
 {
     constexpr int kArrays = kBack && !kMapsOnly ? 3 : 2, kOut = kMapsOnly ? 0 : kBack ? 2 : 1;
-    constexpr int kChunk = kRun * kRuns, kStages = stages_of(kBack, kMapsOnly, kTma);
+    constexpr bool kTma = kWay == kByTma;
+    constexpr int kChunk = kRun * kRuns, kStages = stages_of(sizeof(T), kBack, kMapsOnly, kTma);
     constexpr int kBytes = chunk_bytes<T, kRun>(kTma);            // of an array's chunk
     constexpr int kBoxes = sizeof(T) / 2, kBox = kBytes / kBoxes;  // of it by TMA; bytes of one
     extern __shared__ uint8_t raw[];
@@ -809,7 +820,7 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
             if constexpr (kTma) {
                 return Tile<T, kRun>{reinterpret_cast<T *>(stage(s)) + place_of<T, kRun>(run_at, channel)};
             } else {
-                Rows<T, kRun, kArrays> rows;
+                Rows<T, kRun, kArrays, kWay == kByPairs> rows;
                 rows.p = stage(s) + (run_at / kRun) * pitch_of<T>() + channel * sizeof(T);
 #pragma unroll
                 for (int k = 0; k < kArrays; ++k) {
@@ -1091,8 +1102,16 @@ __global__ __launch_bounds__(256) void step_kernel(const Args a)
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Steps of a run: no more than the sequence has, eight of 32-bit values (two
-// blocks' chunks of 16 would not fit shared memory).
-int run_of(int64_t T, int e) { return T <= 4 * kRuns ? 4 : T <= 8 * kRuns || e == 4 ? 8 : kLongRun; }
+// blocks' chunks of 16 would not fit shared memory).  Of 16-bit values 16 are
+// faster (62 us against 65 on 128 steps, 98 against 135 on 4,096) but where
+// half of the last of few chunks would be empty (129 steps: 151 against 113).
+int run_of(int64_t T, int e)
+{
+    if (T <= 4 * kRuns)
+        return 4;
+    const int64_t rest = T % (kLongRun * kRuns);
+    return T <= 8 * kRuns || e == 4 || (T < 1024 && rest > 0 && rest <= 8 * kRuns) ? 8 : kLongRun;
+}
 int64_t chunks_of(int64_t T, int e) { return up(T, run_of(T, e) * kRuns); }
 
 // Blocks of channels: numbered through where the sequences lie side by side.
@@ -1152,12 +1171,18 @@ cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
         tma = tma && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && t * (int64_t)sizeof(T) % 16 == 0 &&
               (a.flat || b * (int64_t)sizeof(T) % 16 == 0);
     };
+    auto in_words = [&](const void *p, int64_t t, int64_t b) {
+        return (reinterpret_cast<uintptr_t>(p) & 3) == 0 && t % 2 == 0 && (a.flat || b % 2 == 0);
+    };
     for (int k = 0; k < kArrays; ++k)
         whole_pieces(a.in[k], a.it[k], a.ib[k]);
     for (int k = 0; k < kOut; ++k) {
         whole_pieces(a.out[k], a.ot[k], a.ob[k]);
-        a.words[k] = (reinterpret_cast<uintptr_t>(a.out[k]) & 3) == 0 && a.ot[k] % 2 == 0 && (a.flat || a.ob[k] % 2 == 0);
+        a.words[k] = in_words(a.out[k], a.ot[k], a.ob[k]);
     }
+    bool words = sizeof(T) == 2;
+    for (int k = 0; k < kArrays; ++k)
+        words = words && in_words(a.in[k], a.it[k], a.ib[k]);
     TensorMaps maps{};
     for (int k = 0; k < kArrays && tma; ++k)
         tma = array_map(&maps.in[k], dtype, a.in[k], n, a.T, kRun, a.it[k], sequences, a.ib[k]);
@@ -1172,16 +1197,21 @@ cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
         kernel<<<(unsigned)grid, kThreads, bytes, st>>>(maps, a);
         return cudaGetLastError();
     };
-    if (segments > 1) {
-        const int stages = stages_of(kBack, true, tma);
-        const cudaError_t e = tma ? run(walk_kernel<T, kBack, true, true, kRun>, stages, 2)
-                                  : run(walk_kernel<T, kBack, true, false, kRun>, stages, 2);
-        if (e != cudaSuccess)
-            return e;
+    auto both = [&](auto way) {
+        if (segments > 1) {
+            const cudaError_t e = run(walk_kernel<T, kBack, true, way.value, kRun>, stages_of(sizeof(T), kBack, true, tma), 2);
+            if (e != cudaSuccess)
+                return e;
+        }
+        return run(walk_kernel<T, kBack, false, way.value, kRun>, stages_of(sizeof(T), kBack, false, tma), kArrays);
+    };
+    if (tma)
+        return both(std::integral_constant<int, kByTma>());
+    if constexpr (sizeof(T) == 2) {
+        if (words)
+            return both(std::integral_constant<int, kByPairs>());
     }
-    const int stages = stages_of(kBack, false, tma);
-    return tma ? run(walk_kernel<T, kBack, false, true, kRun>, stages, kArrays)
-               : run(walk_kernel<T, kBack, false, false, kRun>, stages, kArrays);
+    return both(std::integral_constant<int, kBySingles>());
 }
 
 template <class T, bool kBack, int kRun>
