@@ -1,4 +1,5 @@
-"""Compile libautoverse.so in-tree for sm_103a (nvcc, no cmake)."""
+"""Compile libautoverse.so in-tree for sm_103a (nvcc, no cmake) and the policy
+operators' binding, _policy.so (g++, against the installed torch)."""
 from __future__ import annotations
 
 import os
@@ -19,6 +20,8 @@ DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "launch.h", "k_
                                                      "variant_keys.cuh", "policy.h", "values.cuh",
                                                      "async.cuh", "tensor_map.h")] + [
     os.path.join(ROOT, "include", "autoverse.h")]
+BINDING = os.path.join(CSRC, "policy_binding.cpp")
+BINDING_LIB = os.path.join(PKG, "_policy.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -27,32 +30,64 @@ def nvcc() -> str:
     return cand if os.path.exists(cand) else "nvcc"
 
 
+def _compile_binding(obj: str) -> list:
+    """The command that compiles the binding."""
+    import sysconfig
+
+    import torch
+    at = os.path.dirname(os.path.abspath(torch.__file__))
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    inc = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={abi}",
+            "-I", os.path.join(ROOT, "include"), *(x for d in inc for x in ("-isystem", d)), "-c", BINDING, "-o", obj]
+
+
+def _link_binding(obj: str, out: str) -> list:
+    import torch
+    libs = os.path.join(os.path.dirname(os.path.abspath(torch.__file__)), "lib")
+    return ["g++", "-shared", obj, "-o", out, "-L", PKG, "-l:libautoverse.so", "-L", libs, "-ltorch_python",
+            "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{libs}"]
+
+
 def build(force: bool = False, verbose: bool = False, extra: list | None = None) -> str:
-    """Build the shared library next to this file: every translation unit is
-    compiled in parallel, then linked.  Returns the library's path."""
-    stale = not os.path.exists(LIB) or any(os.path.getmtime(d) > os.path.getmtime(LIB) for d in DEPS)
-    if not (force or stale or extra):
+    """Build the shared library and the binding next to this file: every
+    translation unit is compiled in parallel, then linked.  Returns the
+    library's path."""
+    def stale(lib, deps):
+        return not os.path.exists(lib) or any(os.path.getmtime(d) > os.path.getmtime(lib) for d in deps)
+
+    native = bool(force or extra) or stale(LIB, DEPS)
+    binding = native or stale(BINDING_LIB, [BINDING, LIB])
+    if not binding:
         return LIB
     import tempfile
     from concurrent.futures import ThreadPoolExecutor
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd))
+        subprocess.check_call(cmd)
+
     cuda_lib = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "lib64")
     common = [nvcc(), "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-lineinfo", *ARCH,
               "-I", os.path.join(ROOT, "include"), *(extra or [])]
     with tempfile.TemporaryDirectory() as tmpdir:
-        objs = [os.path.join(tmpdir, os.path.basename(src) + ".o") for src in SOURCES]
-        cmds = [common + ["-c", src, "-o", obj] for src, obj in zip(SOURCES, objs)]
-        if verbose:
-            for cmd in cmds:
-                print(" ".join(cmd))
+        sources = SOURCES if native else []
+        objs = [os.path.join(tmpdir, os.path.basename(src) + ".o") for src in sources]
+        glue = os.path.join(tmpdir, "policy_binding.o")
+        cmds = [common + ["-c", src, "-o", obj] for src, obj in zip(sources, objs)] + [_compile_binding(glue)]
         with ThreadPoolExecutor(max_workers=len(cmds)) as pool:
-            list(pool.map(subprocess.check_call, cmds))
-        tmp = LIB + f".tmp{os.getpid()}"
-        link = [nvcc(), "-shared", *ARCH, "-cudart", "shared", "-Xlinker", "-rpath", "-Xlinker", cuda_lib,
-                *objs, "-o", tmp]
-        if verbose:
-            print(" ".join(link))
-        subprocess.check_call(link)
-    os.replace(tmp, LIB)
+            list(pool.map(run, cmds))
+        if native:
+            tmp = LIB + f".tmp{os.getpid()}"
+            run([nvcc(), "-shared", *ARCH, "-cudart", "shared", "-Xlinker", "-rpath", "-Xlinker", cuda_lib,
+                 "-Xlinker", "-soname", "-Xlinker", os.path.basename(LIB), *objs, "-o", tmp])
+            os.replace(tmp, LIB)
+        tmp = BINDING_LIB + f".tmp{os.getpid()}"
+        run(_link_binding(glue, tmp))
+        os.replace(tmp, BINDING_LIB)
     return LIB
 
 
