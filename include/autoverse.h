@@ -413,9 +413,10 @@ int av_layer_norm_work(int64_t rows, int32_t n, int64_t *bytes);
  * state after step T - 1 (unrounded), or NULL; it may be h0 itself.
  * states: float [av_scan_sizes' states], kept for av_scan_grad, or NULL.
  * work: av_scan_sizes' work bytes, 16-byte aligned (may be NULL when 0).
- * Long sequences are split over blocks that wait for their predecessors'
- * states.  Each wait has a limit of some seconds; past it the block writes
- * NaN in place of its outputs, so that no wrong state passes for a right one. */
+ * Long sequences of few channels are cut into segments, whose inputs are read
+ * twice; no block waits for another.  A block's wait for its own copies has a
+ * limit of some seconds; past it the block writes NaN in place of its outputs,
+ * so that no wrong state passes for a right one. */
 int av_scan(int64_t T, int64_t B, int64_t D, int32_t dtype, const void *gate, int64_t gate_t,
             int64_t gate_b, const void *value, int64_t value_t, int64_t value_b,
             const uint8_t *reset, int64_t reset_t, int64_t reset_b, const float *h0, void *h,

@@ -23,8 +23,8 @@
 // fill the GPU, a sequence is cut into segments: a first pass makes every
 // segment's map, a second walks the segments from the states that the maps
 // before them give, in one order.  The inputs are read twice then, but no block
-// waits for another.  Up to eight steps (16 of 32 bits) of many channels take a thread each for
-// two channels.
+// waits for another.  Up to eight steps (16 of 32 bits) of many channels take a
+// thread for two channels.
 //
 // A step that begins an episode forgets the state even where it is NaN: in a
 // map this is a factor with its sign bit set, which survives composition.

@@ -3,8 +3,9 @@
 // Argument marshalling between torch tensors and the library's C functions:
 // checks what it is given (ValueError), makes the outputs, takes the current
 // stream, calls av_*.  It is written against torch's C++ interface because on
-// small inputs a call's time is the host's: through ctypes and torch's Python
-// functions a layer norm of one row took 15 us, three of them the launch.
+// small inputs a call's time is the host's: a layer norm of one row of 256 took
+// 17.3 us through ctypes and torch's Python functions and takes 5.9 here, some
+// four of them the library's call.
 // The functions take positional arguments only; policy.py is their face.
 #include <ATen/cuda/EmptyTensor.h>
 #include <Python.h>
