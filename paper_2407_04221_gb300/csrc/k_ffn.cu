@@ -63,6 +63,8 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t 
 {
     const int lane = threadIdx.x & 31;
     const int64_t j = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
+    if constexpr (kGrad)
+        next_may_start();
     if (j >= H)
         return;
     const T *wg = w + j * D, *wu = w + (H + j) * D;
@@ -333,6 +335,8 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
     cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(tmem_at);
+    next_may_start();
+    after_previous();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -530,6 +534,8 @@ template <class T>
 __global__ void ffn_parts_kernel(int64_t rows, int64_t cols, int splits, const float *parts, T *out, int64_t os)
 {
     const int64_t per = cols / 4, n = rows * per;
+    next_may_start();
+    after_previous();
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
         float4 v = reinterpret_cast<const float4 *>(parts)[i];
         for (int s = 1; s < splits; ++s) {
@@ -585,15 +591,16 @@ int64_t parts_bytes(int64_t m, int64_t n, int64_t k)
 int64_t dgu_bytes(int64_t rows, int64_t H) { return up(rows * 2 * H * 2, 256) * 256; }
 
 template <class T, int kForm, int kAct, bool kParts>
-cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Params &p, cudaStream_t st)
+cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Params &p, cudaStream_t st,
+               bool chained)
 {
     const auto kernel = ffn_kernel<T, kForm, kAct, kParts>;  // (kAct plays no part in the last two forms)
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(kForm));
     if (e != cudaSuccess)
         return e;
     const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles * p.splits;
-    kernel<<<2 * (unsigned)(tiles < kPairs ? tiles : kPairs), threads_of(kForm), smem_of(kForm), st>>>(a, b, out, p);
-    return cudaGetLastError();
+    return launch_chained(kernel, 2 * (unsigned)(tiles < kPairs ? tiles : kPairs), threads_of(kForm), smem_of(kForm), st,
+                          chained, a, b, out, p);
 }
 
 // out [m][n] = A B, in one go or in parts.
@@ -615,19 +622,18 @@ cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64
         const int box[3] = {64, kRowsCta, 1};
         if (!make_map(&map, dtype, out, 3, dims, strides, box))
             return cudaErrorInvalidValue;
-        return go<T, kForm, AV_SILU, false>(a, b, map, p, st);
+        return go<T, kForm, AV_SILU, false>(a, b, map, p, st, true);
     }
     const int64_t strides[2] = {n, m * n};
     const int box[3] = {32, kRowsCta, 1};
     if (!make_map(&map, AV_F32, parts, 3, dims, strides, box))
         return cudaErrorInvalidValue;
-    cudaError_t e = go<T, kForm, AV_SILU, true>(a, b, map, p, st);
+    cudaError_t e = go<T, kForm, AV_SILU, true>(a, b, map, p, st, true);
     if (e != cudaSuccess)
         return e;
     const int64_t blocks = up(m * n / 4, 256);
-    ffn_parts_kernel<T><<<(unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 256, 0, st>>>(m, n, p.splits, parts, (T *)out,
-                                                                                      m > 1 ? os : n);
-    return cudaGetLastError();
+    return launch_chained(ffn_parts_kernel<T>, (unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 256, 0, st, true, m, n,
+                          p.splits, parts, (T *)out, m > 1 ? os : n);
 }
 
 template <class T, int kAct, bool kGrad>
@@ -667,7 +673,7 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
     if (!operand_map(&a, dtype, x, rows, D, xs, kRowsCta) || !operand_map(&b, dtype, w, 2 * H, D, D, kRowsCta) ||
         !make_map(&out, dtype, kGrad ? dgu : h, 3, dims, strides, box))
         return cudaErrorInvalidValue;
-    return go<T, kGrad ? kProjGrad : kForward, kAct, false>(a, b, out, p, st);
+    return go<T, kGrad ? kProjGrad : kForward, kAct, false>(a, b, out, p, st, false);
 }
 
 }  // namespace

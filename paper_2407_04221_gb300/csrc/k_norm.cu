@@ -288,6 +288,7 @@ __global__ __launch_bounds__(kMost, kMin) void norm_grad_kernel(int64_t rows, in
                                                                 const float *mean, const float *rstd, T *dx,
                                                                 int64_t dxs, float *parts)
 {
+    next_may_start();
     constexpr int kPacks = kPer / kVec, kPairs = kPer / 2;
     constexpr bool kHeld = kMost < 1024 || kPer <= 8;
     using P = Params<kVec, kPer>;
@@ -619,6 +620,7 @@ __global__ __launch_bounds__(kMost, kMin) void norm_grad_ring_kernel(int64_t row
                                                                      const float *rstd, T *dx, int64_t dxs,
                                                                      float *parts, int deep)
 {
+    next_may_start();
     constexpr int kPacks = kPer / kVec, kPairs = kPer / 2;
     constexpr bool kKeep = sizeof(T) == 2 && kMin == 1;  // xh and d are kept: of 16 bits they are dear to make again
     using P = Params<kVec, kPer>;
@@ -820,6 +822,7 @@ __global__ __launch_bounds__(256) void norm_long_columns_kernel(int64_t rows, in
                                                                 const T *x, int64_t xs, const float *mean,
                                                                 const float *rstd, float *parts)
 {
+    next_may_start();
     __shared__ float s[2][8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     const int64_t r0 = rows * blockIdx.y / gridDim.y, r1 = rows * (blockIdx.y + 1) / gridDim.y;
@@ -853,6 +856,7 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(int count, int n, con
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * kColumns + lane;
     const float *from = parts + (blockIdx.y ? n : 0);
     void *to = blockIdx.y ? db : dw;
+    after_previous();
     if (!to)
         return;
     float v = 0.0f;
@@ -1174,9 +1178,9 @@ cudaError_t launch_norm_grad(int64_t rows, int n, int dtype, int param_dtype, co
             return e;
     }
     if (sums)
-        norm_columns_kernel<<<dim3((n + kColumns - 1) / kColumns, 2), 256, 0, st>>>(count, n, parts, param_dtype,
-                                                                                   dweight, dbias);
-    return cudaGetLastError();
+        return launch_chained(norm_columns_kernel, dim3((n + kColumns - 1) / kColumns, 2), 256, 0, st, rows > 0, count, n,
+                              parts, param_dtype, dweight, dbias);
+    return cudaSuccess;
 }
 
 }  // namespace av

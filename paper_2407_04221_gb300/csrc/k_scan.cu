@@ -788,6 +788,10 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
         order.next(a, items[1]);
     }
     __syncthreads();
+    if constexpr (kMapsOnly)
+        next_may_start();
+    else
+        after_previous();
     fill(items[0], 0);
     bool ok = true;
     uint32_t phases = 0;
@@ -1189,21 +1193,21 @@ cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
     for (int k = 0; k < kOut && tma; ++k)
         tma = array_map(&maps.out[k], dtype, a.out[k], n, a.T, kRun, a.ot[k], sequences, a.ob[k]);
     const int64_t units = slabs * segments, grid = units < resident ? units : resident;
-    auto run = [&](auto kernel, int stages, int arrays) {
+    auto run = [&](auto kernel, int stages, int arrays, bool chained) {
         const int bytes = stages * arrays * chunk_bytes<T, kRun>(tma) + 1024;
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess)
             return e;
-        kernel<<<(unsigned)grid, kThreads, bytes, st>>>(maps, a);
-        return cudaGetLastError();
+        return launch_chained(+kernel, (unsigned)grid, kThreads, bytes, st, chained, maps, a);
     };
     auto both = [&](auto way) {
         if (segments > 1) {
-            const cudaError_t e = run(walk_kernel<T, kBack, true, way.value, kRun>, stages_of(sizeof(T), kBack, true, tma), 2);
+            const cudaError_t e = run(walk_kernel<T, kBack, true, way.value, kRun>, stages_of(sizeof(T), kBack, true, tma), 2, false);
             if (e != cudaSuccess)
                 return e;
         }
-        return run(walk_kernel<T, kBack, false, way.value, kRun>, stages_of(sizeof(T), kBack, false, tma), kArrays);
+        return run(walk_kernel<T, kBack, false, way.value, kRun>, stages_of(sizeof(T), kBack, false, tma), kArrays,
+                   segments > 1);
     };
     if (tma)
         return both(std::integral_constant<int, kByTma>());
