@@ -899,8 +899,8 @@ Shape shape_for(int n, int per, int several, int most, int resident)
     return s;
 }
 
-// Rows that go through registers: of up to a kilobyte, and backward beyond
-// 8,192 values.  wide: 16-bit values, eight at a time.
+// Rows that go through registers: those that are not `ringed`.  wide: 16-bit
+// values, eight at a time.
 Shape shape_of(int n, bool wide, bool back)
 {
     if (n > 1024)
@@ -910,11 +910,14 @@ Shape shape_of(int n, bool wide, bool back)
     return shape_for(n, 8, 512, 512, 2);
 }
 
-// Whether rows go by bulk copies (where these are of a kilobyte or more), and
-// then how.
+// Whether rows go by bulk copies: where these are of a kilobyte or more (a group
+// is of whole warps then).  Through registers 32,768 rows of 1,024 16-bit values
+// take 55 us and by copies 31, 65,536 of 1,001 32-bit ones, which do not start
+// on 16 bytes, 131 and 103; but those of 1,024, in whole packs, 86 and 99 (the
+// gradient 128 and 130, of 384 136 and 150).
 bool ringed(int n, int e, bool wide, bool back)
 {
-    return n * e > 1024 && n <= (back ? 8192 : kLongest);
+    return n * e > 1024 && !(e == 4 && wide && n <= 1024) && n <= (back ? 8192 : kLongest);
 }
 Shape ring_of(int n, bool wide, bool back)
 {
