@@ -30,9 +30,7 @@ constexpr int kTiny = 8;           // entries of a row that a thread takes
 constexpr int kTinyThreads = 128;
 constexpr int kNarrow = 1024;      // entries of a row that a group of lanes takes
 constexpr int kNarrowThreads = 256;
-constexpr int kMiddle = 8192;      // entries of a row that a block of 128 threads takes; longer ones one of 512
 constexpr int kGradThreads = 256;
-constexpr int kGradWarp = 4096;    // entries of a row whose gradient a warp takes
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -700,6 +698,19 @@ void with_lanes(int V, F f)
         f(integral_constant<int, 32>(), integral_constant<int, 32>());
 }
 
+// Whether rows take a block of 128 threads (else one of 512): many of them, of
+// up to 32 KB.  Of 16-bit entries, small block and large: 4,864 rows of 2,000 11
+// and 24 us, of 16,384 34 and 44, with four alternatives 50 and 62; 608 of 2,000
+// 4.6 and 6.5, of 8,192 6.7 and 8.5; but 304 of 8,192 with alternatives 10.8 and
+// 8.5, 608 of 12,000 13.1 and 11.9, 2,432 of 24,000 44 and 40.
+bool small_blocks(int64_t rows, int64_t bytes) { return bytes <= 32768 && rows >= (bytes <= 16384 ? 608 : 1216); }
+
+// Whether a row's gradient takes a warp (else blocks, of 16,384 entries each):
+// 4,864 rows of 4,096 16-bit entries take 15 us by warps and 22 by blocks, 2,432
+// of 8,192 15.6 and 16.9, of 2,000 32-bit ones 9.0 and 10.7; but 608 of 1,500 6.7
+// and 5.6, 304 of 8,192 11.0 and 6.4, 2,432 of 8,192 32-bit ones 32 and 29.
+bool by_warps(int64_t rows, int64_t bytes) { return bytes <= 16384 && rows >= 1216; }
+
 // Rows of whole 16-byte packs.
 bool packs(const void *p, int64_t rows, int V, int64_t stride, int64_t e)
 {
@@ -738,7 +749,7 @@ cudaError_t launch_logp(const LogpArgs &a, int top, float *logp, float *entropy,
                     kernel<<<(unsigned)(a.rows < most ? a.rows : most), threads, 0, st>>>(a, top, logp, entropy, peak,
                                                                                          logz, top_logp, top_index);
                 };
-                if (a.V <= kMiddle && a.rows >= 152)
+                if (small_blocks(a.rows, a.V * (int64_t)sizeof(T)))
                     run(logp_wide_kernel<T, 128, mask.value, tops.value>, 128);
                 else
                     run(logp_wide_kernel<T, 512, mask.value, tops.value>, 512);
@@ -756,13 +767,15 @@ cudaError_t launch_logp_grad(const LogpArgs &a, const float *dlogp, const float 
         using T = decltype(v);
         T *dx = (T *)dlogits;
         const int64_t e = sizeof(T);
-        if (a.V > kTiny && a.V <= kNarrow) {
+        const bool whole = packs(a.logits, a.rows, a.V, a.stride, e) && packs(dlogits, a.rows, a.V, dlogit_stride, e);
+        // (two lanes for eight 32-bit entries: 44 us for 2 M rows, a thread for them 72; of 16 bits 52 and 50)
+        if (a.V <= kNarrow && (a.V > kTiny || (whole && a.V * e >= 32))) {
             with_lanes(a.V, [&](auto lanes, auto per) {
                 auto run = [&](auto kernel) {
                     kernel<<<(unsigned)up(a.rows * lanes.value, kNarrowThreads), kNarrowThreads, 0, st>>>(
                         a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride);
                 };
-                if (packs(a.logits, a.rows, a.V, a.stride, e) && packs(dlogits, a.rows, a.V, dlogit_stride, e))
+                if (whole)
                     run(logp_narrow_grad_kernel<T, 16 / sizeof(T), lanes.value, per.value>);
                 else
                     run(logp_narrow_grad_kernel<T, 1, lanes.value, per.value>);
@@ -776,7 +789,7 @@ cudaError_t launch_logp_grad(const LogpArgs &a, const float *dlogp, const float 
             if (a.V <= kTiny) {
                 logp_grad_tiny_kernel<T, mask.value><<<(unsigned)up(a.rows, kTinyThreads), kTinyThreads, 0, st>>>(
                     a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride);
-            } else if (a.V <= kGradWarp) {
+            } else if (by_warps(a.rows, a.V * e)) {
                 logp_wide_grad_kernel<T, 32, mask.value>
                     <<<(unsigned)up(a.rows, kGradThreads / 32), kGradThreads, 0, st>>>(
                         a, dlogp, dentropy, peak, logz, entropy, dx, dlogit_stride, packed);
