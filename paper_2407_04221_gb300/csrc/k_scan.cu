@@ -44,7 +44,10 @@ constexpr int kLongRun = 16;     // steps of a run at most
 constexpr int kSlab = 64;        // channels of a block, eight a warp, two a lane
 constexpr int kSms = 152;
 constexpr int kMaps = 32;        // maps of a block: a pair of channels each
-constexpr int64_t kBriefChannels = 4096;  // from where on brief sequences take a thread for two channels
+// From where on brief sequences take a thread for two channels: of 16,384 four
+// steps take 4.6 us so and 6.5 walked, eight 6.7 and 6.5 (backward 6.7 and 8.5),
+// of 131,072 channels eight 6.7 and 19.8.
+constexpr int64_t kBriefChannels = 4096;
 
 __device__ __forceinline__ float exp2_fast(float v)
 {
@@ -1121,11 +1124,16 @@ int64_t chunks_of(int64_t T, int e) { return up(T, run_of(T, e) * kRuns); }
 // Blocks of channels: numbered through where the sequences lie side by side.
 int64_t slabs_of(int64_t B, int64_t D, bool flat) { return flat ? up(B * D, kSlab) : B * up(D, kSlab); }
 
-// Segments of a sequence: one where the channels fill more than half of what
-// the GPU holds (cutting reads the inputs twice), else what fills it.
+// Segments of a sequence: one where the channels fill more than a third of what
+// the GPU holds (cutting reads the inputs twice), else what fills it.  Of 4,096
+// steps of 16-bit values, whole and cut: 64 slabs 60 and 39 us, 100 60 and 52 (of
+// 304 blocks), 120 60 and 71; of 32 bits 150 111 and 108 (of 456), 200 137 and 152.
+// Few chunks are cut where there are few channels: of four, 4 slabs 10.5 and 8.8
+// us (backward 16.7 and 10.6), 32 10.6 and 10.5 (16.7 and 12.6), 90 10.8 and 14.7
+// (16.7 and 19.2); of two, 4 slabs 8.5 and 8.6.
 int64_t segments_of(int64_t slabs, int64_t chunks, int64_t resident)
 {
-    if (2 * slabs > resident || chunks <= 4)
+    if (3 * slabs > resident || chunks <= 3 || (chunks <= 6 && 8 * slabs > resident))
         return 1;
     const int64_t most = resident / slabs, per = up(chunks, most < chunks ? most : chunks);
     return up(chunks, per);
