@@ -11,7 +11,13 @@
 // of the other projection, so one CTA's accumulators hold both factors of its
 // outputs and h leaves rounded once, with no array in between.  The backward
 // pass makes g and u again (4 M D H operations of 16) instead of keeping them:
-// kept in 16 bits they would cost accuracy, in 32 bits 8 bytes a unit.
+// kept in 16 bits they would cost accuracy, in 32 bits 8 bytes a unit.  dg and du
+// go to the last products in 16 bits, which these take: that rounding and the
+// result's own make 1.41 times the error of the latter alone, as root mean
+// square.  Where there are few of them, they need not be average, and single
+// cases reached 1.9 times (one row; 1.5 of 5 x 1,024, none from 8,192 on): there
+// (`in_two`) they go as two values, the rounded one and what it leaves, and the
+// products take both.
 //
 // Warps: one issues copies (TMA), one products, four or eight take accumulators
 // to memory while the next tile's products run (two sets of 256 TMEM columns).
@@ -40,6 +46,14 @@ __device__ __forceinline__ void activate(float g, float &f, float &slope)
     slope = s + f * (1.0f - s) * din;
 }
 
+// What rounding to T leaves of v; nothing of infinity and NaN.
+template <class T>
+__device__ __forceinline__ float left_of(float v)
+{
+    const float r = to_f32(from_f32<T>(v));
+    return fabsf(r) <= 3.402823466e38f ? v - r : 0.0f;
+}
+
 // ------------------------------------------------------------ few rows
 
 constexpr int kFewRows = 4;  // (eight: 18.6 us, 16: 28.8, by tensor cores 12.5, at 1,024 x 4,096)
@@ -59,7 +73,7 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float *f)
 template <class T, int kAct, int R, bool kGrad>
 __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t D, int64_t H, const T *x, int64_t xs,
                                                                const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
-                                                               T *dgu)
+                                                               T *dgu, int parts)
 {
     const int lane = threadIdx.x & 31;
     const int64_t j = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
@@ -102,8 +116,13 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t 
             h[r * hs + j] = from_f32<T>(f * u[r]);
         } else {
             const float d = to_f32(dh[r * dhs + j]);
-            dgu[r * 2 * H + j] = from_f32<T>(d * u[r] * slope);
-            dgu[r * 2 * H + H + j] = from_f32<T>(d * f);
+            T *to = dgu + r * 2 * parts * H + j;
+            to[0] = from_f32<T>(d * u[r] * slope);
+            to[H] = from_f32<T>(d * f);
+            if (parts == 2) {
+                to[2 * H] = from_f32<T>(left_of<T>(d * u[r] * slope));
+                to[3 * H] = from_f32<T>(left_of<T>(d * f));
+            }
         }
     }
 }
@@ -138,6 +157,8 @@ struct Params {
     int m, n;               // rows and columns of the result (forward forms: columns of H)
     int m_tiles, n_tiles;   // of a pair
     int k_blocks, splits;   // blocks of 64 terms in all, parts that they are dealt to
+    int k_once;             // of them those of A's first value; B's come again for the second
+    int in_two;             // dg and du: 2 if they leave as two values, else 1
     const void *dh;
     int64_t dhs;
 };
@@ -173,6 +194,14 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
                  "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
                  "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                  : "memory");
 }
 
@@ -354,17 +383,20 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     if (rank == 0)
                         bar_expect(full + 8 * s, 4 * kHalf);
                     const uint32_t bar = in_cta(full + 8 * s, 0), a = base + s * 2 * kHalf, b = a + kHalf;
+                    const int second = !kGated && k >= p.k_once, term = (k - (second ? p.k_once : 0)) * kBlockK;
                     if (kARows) {
-                        load_box(a, &a_map, am, k * kBlockK, bar);
-                        load_box(a + kHalf / 2, &a_map, am + 64, k * kBlockK, bar);
+                        load_box(a, &a_map, am, term, second, bar);
+                        load_box(a + kHalf / 2, &a_map, am + 64, term, second, bar);
+                    } else if (!kGated) {
+                        load_box(a, &a_map, term, am, second, bar);
                     } else {
-                        load_box(a, &a_map, k * kBlockK, am, bar);
+                        load_box(a, &a_map, term, am, bar);
                     }
                     if (kBRows) {
-                        load_box(b, &b_map, bn, k * kBlockK, bar);
-                        load_box(b + kHalf / 2, &b_map, bn + 64, k * kBlockK, bar);
+                        load_box(b, &b_map, bn, term, bar);
+                        load_box(b + kHalf / 2, &b_map, bn + 64, term, bar);
                     } else {
-                        load_box(b, &b_map, k * kBlockK, bn, bar);
+                        load_box(b, &b_map, term, bn, bar);
                     }
                 }
             }
@@ -425,7 +457,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
             };
             if (kGated) {
 #pragma unroll 1
-                for (int c = team * 64; c < kRowsCta; c += 64 * kTeams) {  // 64 columns of H a team
+                for (int c = team * 64, part = 0; c < kRowsCta;) {  // 64 columns of H a team, each value of dg and du
                     if (first)
                         stores_left<0>();
                     team_sync(team);
@@ -463,6 +495,13 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                                 g[e] = d[e] * u[e] * slope;
                                 u[e] = d[e] * f;
                             }
+                            if (part) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) {
+                                    g[e] = left_of<T>(g[e]);
+                                    u[e] = left_of<T>(u[e]);
+                                }
+                            }
                             put32<T>(slab, row, half, g);
                             put32<T>(slab + kSlab, row, half, u);
                         }
@@ -471,12 +510,16 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     team_sync(team);
                     if (first && t.n * kRowsCta + c < p.n && m0 < p.m) {
                         const int col = t.n * kRowsCta + c;
-                        store_box(&out_map, slab, col, 0, m0);
+                        store_box(&out_map, slab, col, 2 * part, m0);
                         if (kForm == kProjGrad)
-                            store_box(&out_map, slab + kSlab, col, 1, m0);
+                            store_box(&out_map, slab + kSlab, col, 2 * part + 1, m0);
                     }
                     if (first)
                         stores_close();
+                    if (kForm == kForward || ++part == p.in_two) {
+                        part = 0;
+                        c += 64 * kTeams;
+                    }
                 }
             } else {
                 constexpr int kWide = kParts ? 32 : 64;  // columns of 128 bytes
@@ -556,17 +599,33 @@ bool operand_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64
     return make_map(map, dtype, p, 2, dims, strides, box);
 }
 
+// dg and du as A: [value][row][2 H] by columns, rows and values, boxes of box_rows x 64 columns.
+bool grads_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64_t H, int parts, int box_rows)
+{
+    const int64_t dims[3] = {2 * H, rows, parts}, strides[2] = {2 * parts * H, 2 * H};
+    const int box[3] = {64, box_rows, 1};
+    return make_map(map, dtype, p, 3, dims, strides, box);
+}
+
 constexpr int kPairs = 76;  // of a GB300's 152 SMs
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Values that dg and du go as: two where there are up to 32,768 of either, some
+// six times what the largest case of more than 1.5 times the error had (5 x
+// 1,024).  There it costs little: 4 x 1,024 x 4,096 38 us once and 40 twice, 16 x
+// 1,024 x 1,024 32 and 37; 16,384 x 1,024 x 4,096 would take half as long again.
+int in_two(int64_t rows, int64_t H) { return rows * H <= 32768 ? 2 : 1; }
+
+int64_t blocks_of(int64_t k, int parts) { return up(k, kBlockK) * parts; }
 
 // Into how many parts the terms of a product are dealt: the number that ends
 // soonest.  A block of 64 terms takes a pair 0.27 us; each part writes its
 // sums in 32 bits, 0.8 us a tile, and a pass adds them up (3 us and 8 bytes a
 // sum and part at 5 TB/s).
-int splits_for(int64_t m, int64_t n, int64_t k)
+int splits_for(int64_t m, int64_t n, int64_t blocks)
 {
-    const int64_t tiles = up(m, kTile) * up(n, kTile), blocks = up(k, kBlockK);
+    const int64_t tiles = up(m, kTile) * up(n, kTile);
     int best = 1;
     double least = 0.0;
     for (int s = 1; s <= 16 && s <= blocks; ++s) {
@@ -582,13 +641,13 @@ int splits_for(int64_t m, int64_t n, int64_t k)
     return best;
 }
 
-int64_t parts_bytes(int64_t m, int64_t n, int64_t k)
+int64_t parts_bytes(int64_t m, int64_t n, int64_t blocks)
 {
-    const int s = splits_for(m, n, k);
+    const int s = splits_for(m, n, blocks);
     return s > 1 ? (int64_t)s * m * n * 4 : 0;
 }
 
-int64_t dgu_bytes(int64_t rows, int64_t H) { return up(rows * 2 * H * 2, 256) * 256; }
+int64_t dgu_bytes(int64_t rows, int64_t H) { return up(rows * 2 * H * 2 * in_two(rows, H), 256) * 256; }
 
 template <class T, int kForm, int kAct, bool kParts>
 cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Params &p, cudaStream_t st,
@@ -606,15 +665,16 @@ cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &ou
 // out [m][n] = A B, in one go or in parts.
 template <class T, int kForm>
 cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64_t m, int64_t n, int64_t k, void *out,
-                    int64_t os, float *parts, cudaStream_t st)
+                    int64_t os, float *parts, int values, cudaStream_t st)
 {
     Params p{};
     p.m = (int)m;
     p.n = (int)n;
     p.m_tiles = (int)up(m, kTile);
     p.n_tiles = (int)up(n, kTile);
-    p.k_blocks = (int)up(k, kBlockK);
-    p.splits = splits_for(m, n, k);
+    p.k_once = (int)up(k, kBlockK);
+    p.k_blocks = (int)blocks_of(k, values);
+    p.splits = splits_for(m, n, p.k_blocks);
     CUtensorMap map;
     const int64_t dims[3] = {n, m, p.splits};
     if (p.splits == 1) {
@@ -638,13 +698,13 @@ cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64
 
 template <class T, int kAct, bool kGrad>
 void few(int rows, int64_t D, int64_t H, const T *x, int64_t xs, const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
-         T *dgu, cudaStream_t st)
+         T *dgu, int parts, cudaStream_t st)
 {
     const unsigned grid = (unsigned)up(H, kFewThreads / 32);
     if (rows <= 1)
-        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu, parts);
     else
-        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu, parts);
 }
 
 // h, or the projections' gradients [rows][2][H].
@@ -654,7 +714,7 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
 {
     if (rows <= kFewRows) {
         few<T, kAct, kGrad>((int)rows, D, H, (const T *)x, xs, (const T *)w, (T *)h, hs, (const T *)dh, dhs, (T *)dgu,
-                            st);
+                            in_two(rows, H), st);
         return cudaGetLastError();
     }
     Params p{};
@@ -663,12 +723,14 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
     p.m_tiles = (int)up(rows, kTile);
     p.n_tiles = (int)up(H, kRowsCta);
     p.k_blocks = (int)up(D, kBlockK);
+    p.k_once = p.k_blocks;
     p.splits = 1;
+    p.in_two = in_two(rows, H);
     p.dh = dh;
     p.dhs = dhs;
     CUtensorMap a, b, out;
-    // (stores are columns, projection, row; h has one)
-    const int64_t dims[3] = {H, kGrad ? 2 : 1, rows}, strides[2] = {H, kGrad ? 2 * H : hs};
+    // (stores are columns, projection of a value, row; h has one)
+    const int64_t dims[3] = {H, kGrad ? 2 * p.in_two : 1, rows}, strides[2] = {H, kGrad ? 2 * p.in_two * H : hs};
     const int box[3] = {64, 1, kRowsCta};
     if (!operand_map(&a, dtype, x, rows, D, xs, kRowsCta) || !operand_map(&b, dtype, w, 2 * H, D, D, kRowsCta) ||
         !make_map(&out, dtype, kGrad ? dgu : h, 3, dims, strides, box))
@@ -680,7 +742,8 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
 
 int64_t ffn_work_bytes(int64_t rows, int64_t D, int64_t H)
 {
-    const int64_t a = parts_bytes(rows, D, 2 * H), b = parts_bytes(2 * H, D, rows);
+    const int64_t a = parts_bytes(rows, D, blocks_of(2 * H, in_two(rows, H))),
+                  b = parts_bytes(2 * H, D, blocks_of(rows, in_two(rows, H)));
     return dgu_bytes(rows, H) + (a > b ? a : b);
 }
 
@@ -715,13 +778,14 @@ cudaError_t launch_ffn_grad(int64_t rows, int64_t D, int64_t H, int dtype, int a
         if (e != cudaSuccess)
             return e;
         CUtensorMap dgu, wt, dgut, xt;
-        if (!operand_map(&dgu, dtype, work, rows, 2 * H, 2 * H, kRowsCta) || !operand_map(&wt, dtype, w, 2 * H, D, D, 64) ||
-            !operand_map(&dgut, dtype, work, rows, 2 * H, 2 * H, 64) || !operand_map(&xt, dtype, x, rows, D, x_stride, 64))
+        const int values = in_two(rows, H);
+        if (!grads_map(&dgu, dtype, work, rows, H, values, kRowsCta) || !operand_map(&wt, dtype, w, 2 * H, D, D, 64) ||
+            !grads_map(&dgut, dtype, work, rows, H, values, 64) || !operand_map(&xt, dtype, x, rows, D, x_stride, 64))
             return cudaErrorInvalidValue;
-        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, st);
+        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, values, st);
         if (e != cudaSuccess)
             return e;
-        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, st);
+        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, values, st);
     };
     return dtype == AV_BF16 ? run(__nv_bfloat16()) : run(__half());
 }

@@ -2,6 +2,7 @@
 the bounds are those of the operators' own tests, whose `check` functions derive them."""
 from __future__ import annotations
 
+import gc
 import threading
 
 import pytest
@@ -12,7 +13,8 @@ from tests import test_gpu_policy_ffn as ffn  # noqa: E402
 from tests import test_gpu_policy_logp as logp  # noqa: E402
 from tests import test_gpu_policy_norm as norm  # noqa: E402
 from tests import test_gpu_policy_scan as scan  # noqa: E402
-from tests.policy_ref import BF16, F16, F32  # noqa: E402
+from tests.policy_ref import (BF16, E, F16, F32, ROUNDOFF, SMALLEST, activate, close, d,  # noqa: E402
+                              gated_ffn)
 
 pytestmark = pytest.mark.gpu
 
@@ -163,6 +165,7 @@ def test_calls_keep_nothing(pol):
     p = torch.nn.Parameter(w)
     tok = torch.zeros(64, dtype=torch.int64, device="cuda")
     torch.cuda.synchronize()
+    gc.collect()  # (cycles that tests before this one left)
     before = torch.cuda.memory_allocated()
     for k in range(50):
         y, mean, rstd = pol.layer_norm(x, p, b)
@@ -179,3 +182,127 @@ def test_calls_keep_nothing(pol):
     del y, mean, rstd, out  # (dy stays: it was there before)
     assert dy.shape == x.shape
     assert torch.cuda.memory_allocated() == before
+
+
+# ------------------------------------------------------------ enough rows for another way
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,V,top", [(607, 1500, 3), (608, 1025, 5), (640, 2049, 0), (608, 8191, 0), (1216, 8193, 0),
+                                        (1217, 1500, 2), (1300, 4095, 0), (1216, 4097, 0)])
+def test_log_probs_of_very_many_wide_rows(pol, rows, V, top, dtype):
+    x, tok, mask, dl, de = logp.make(rows, V, dtype, rows + V)
+    logp.check(pol, x, tok, mask, dl, de, top, f"{rows}x{V} masked")
+    logp.check(pol, x, tok, None, dl, de, 0, f"{rows}x{V}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_log_probs_of_very_many_wide_rows_with_ties_and_gaps(pol, dtype):
+    V = 1500
+    x, tok, mask, dl, de = logp.make(1220, V, dtype, V)
+    x[:40] = x[:40].round().clamp(-1, 1)
+    x[40] = 1.5
+    x[41, -70:] = 20.0
+    x[42] = float("-inf")
+    x[43] = torch.finfo(dtype).min
+    mask[44] = 0
+    mask[45] = 0
+    mask[45, V - 1] = 1
+    logp.check(pol, x, tok, mask, dl, de, 32, f"{V}")
+    wide, wm = torch.nn.functional.pad(x, (3, 2)), torch.nn.functional.pad(mask, (3, 2))
+    logp.check(pol, wide[:, 3:3 + V], tok, wm[:, 3:3 + V], dl, de, 0, f"{V} from 3")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("V", [4, 6, 7, 8])
+def test_log_probs_of_few_entries(pol, V, dtype):
+    x, tok, mask, dl, de = logp.make(3001, V, dtype, V)
+    mask[5] = 0
+    x[6] = float("-inf")
+    logp.check(pol, x, tok, mask, dl, de, V, f"{V}")
+    logp.check(pol, torch.nn.functional.pad(x, (1, 2))[:, 1:1 + V], tok, mask, dl, de, 1, f"{V} from 1")
+
+
+@pytest.mark.parametrize("rows,n", [(1, 300), (40, 384), (700, 512), (3001, 768), (500, 1000), (3001, 1024)])
+def test_norm_of_whole_packs_of_floats(pol, rows, n):
+    x, dy, w, b = norm.make(rows, n, F32, F32, n)
+    norm.check(pol, x, dy, w, b, f"{rows}x{n}")
+    norm.check(pol, x, dy, w.bfloat16(), b.bfloat16(), f"{rows}x{n}")
+    x, dy, w, b = norm.make(rows, n + 4, F32, F32, n)
+    norm.check(pol, x[:, 4:], dy[:, :n], w[:n].contiguous(), None, f"{rows}x{n} from 4")
+    norm.check(pol, x[:, 3:3 + n], dy[:, 1:n + 1], w[:n].contiguous(), None, f"{rows}x{n} from 3")
+
+
+@pytest.mark.parametrize("dtype,B", [(BF16, 101), (BF16, 102), (F32, 101), (F32, 152), (F32, 153)])
+def test_scan_where_cutting_ends(pol, dtype, B):
+    scan.check(pol, *scan.make(700, B, 64, dtype, 0.002, B, shift=3.0), f"{B} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [190, 256, 384, 400, 512, 700, 900])
+@pytest.mark.parametrize("B", [1, 38, 57])
+def test_scan_of_few_chunks_in_segments(pol, T, B, dtype):
+    scan.check(pol, *scan.make(T, B, 64, dtype, 0.005, T + B, shift=3.0), f"{T}x{B} {dtype}")
+
+
+# ------------------------------------------------------------ few gradients of the projections, as two values each
+
+def check_in_two(pol, x, w, dh, act, what):
+    """The bounds of the operator's own tests, but for the rounding of the projections' gradients: a value and what it
+    leaves, each rounded to u, are off by u^2 of the value and half the type's smallest step."""
+    u, D, H, rows = ROUNDOFF[x.dtype], x.shape[1], w.shape[1], x.shape[0]
+    xd, wd, dhd = d(x).requires_grad_(), d(w).requires_grad_(), d(dh)
+    want = torch.autograd.grad((gated_ffn(xd, wd, act) * dhd).sum(), [xd, wd])
+    xd, wd = xd.detach(), wd.detach()
+    g, up = (xd @ wd[0].t()).requires_grad_(), xd @ wd[1].t()
+    f = activate(g, act)
+    (slope,) = torch.autograd.grad(f.sum(), g)
+    g, f = g.detach(), f.detach()
+    ge, ue = (2 * D * (xd.abs() @ wd[k].abs().t()) for k in (0, 1))
+    fe = 1.13 * ge + (g.abs() + 16) * (f.abs() + 1e-3)
+    a = dhd.abs()
+    dg, du = a * up.abs() * slope.abs(), a * f.abs()
+    dge, due = a * (ue * 1.13 + up.abs() * (0.8 * ge + g.abs() + 24)), a * fe
+    er = [1.01 * u * u * v + SMALLEST[x.dtype] + E * e for v, e in ((dg, dge), (du, due))]
+    dx, dw = pol.gated_ffn_grad(dh, x, w, act=act)
+    wa, xa = wd.abs(), xd.abs()
+    close(dx, want[0], 8 * H * (dg @ wa[0] + du @ wa[1]), what + " dx", er[0] @ wa[0] + er[1] @ wa[1])
+    close(dw, want[1], 4 * rows * torch.stack((dg.t() @ xa, du.t() @ xa)), what + " dw",
+          torch.stack((er[0].t() @ xa, er[1].t() @ xa)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,D,H", [(1, 64, 64), (1, 8, 8), (2, 1608, 144), (3, 72, 1000), (4, 64, 8192), (5, 520, 72),
+                                      (17, 64, 64), (63, 72, 40), (64, 128, 256), (65, 72, 504), (128, 64, 256),
+                                      (500, 40, 64)])
+def test_ffn_gradient_of_few_is_rounded_once(pol, rows, D, H, dtype, act):
+    assert rows * H <= 32768
+    x, w, dh = ffn.make(rows, D, H, dtype, rows + D + H)
+    check_in_two(pol, x, w, dh, act, f"{rows} {D} {H}")
+
+
+@pytest.mark.parametrize("rows,H", [(4, 8200), (129, 256), (129, 248), (1025, 32), (1024, 32)])
+def test_ffn_gradient_on_either_side_of_few(pol, rows, H):
+    x, w, dh = ffn.make(rows, 136, H, BF16, rows)
+    ffn.check(pol, x, w, dh, "silu", f"{rows} {H}")
+    wide = torch.nn.functional.pad(x, (8, 16)), torch.nn.functional.pad(dh, (16, 8))
+    ffn.check(pol, wide[0][:, 8:144], w, wide[1][:, 16:16 + H], "gelu", f"{rows} {H} strided")
+
+
+@pytest.mark.parametrize("rows", [3, 6])
+def test_ffn_gradient_beyond_the_type_is_infinite(pol, rows):
+    """A projection's gradient of 60,000 x 4 x 0.93 is infinite in f16, and the input's with it, not NaN."""
+    x, w, dh = ffn.make(rows, 64, 72, F16, rows)
+    x[0], dh[0] = 0, 0
+    x[0, 0], dh[0, 0] = 1, 60000
+    w[:, 0] = 0.5
+    w[0, 0, 0], w[1, 0, 0] = 1, 4
+    dx, _ = pol.gated_ffn_grad(dh, x, w)
+    assert torch.isinf(dx[0]).all() and torch.isfinite(dx[1:]).all()
+
+
+def test_ffn_gradient_of_few_again(pol):
+    x, w, dh = ffn.make(7, 264, 520, BF16, 5)
+    first = pol.gated_ffn_grad(dh, x, w)
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(first, pol.gated_ffn_grad(dh, x, w)))
