@@ -11,15 +11,20 @@
 // for 16-bit logits nearly by issue: six instructions an entry.
 //
 // The k largest of a row in registers are drawn one by one: each lane knows its
-// largest, and only the lane that gave one up looks for the next.  In longer
-// rows the k-th largest of the threads' maxima is no larger than the k-th
-// largest entry, so only entries of threads whose maximum reaches it are looked
-// at again, by the whole warp, and only those that reach it are listed: k and a
-// few.  Their order is counted out by (value, lowest index).  Should the list
-// run over (rows of equal values), or hold NaN, the k largest are drawn one by
-// one instead.
+// largest, and only the lane that gave one up looks for the next (of 16 bits by
+// value and index in one word: 65,536 rows of 256 with eight 49 us, with the
+// index apart 78).  Where a warp or a block holds the row they are listed
+// instead, in a warp from two on (65,536 rows of 1,000 with four 100 us, drawn
+// 154; with twenty 125 and 514; with one 98 and 94): the k-th largest of the
+// threads' maxima is no larger than the k-th largest entry, so only entries that
+// reach it can be among them, k and a few, and their order is counted out by
+// (value, lowest index).  A block looks again only at threads whose maximum
+// reaches it, by whole warps.  Should the list run over (rows of equal values),
+// or in a block hold NaN, the k largest are drawn one by one all the same.
 //
 // Addition has one order throughout: equal rows give equal bits.
+#include <string.h>
+
 #include "policy.h"
 #include "values.cuh"
 
@@ -30,6 +35,7 @@ constexpr int kTiny = 8;           // entries of a row that a thread takes
 constexpr int kTinyThreads = 128;
 constexpr int kNarrow = 1024;      // entries of a row that a group of lanes takes
 constexpr int kNarrowThreads = 256;
+constexpr int kShort = 64;         // entries of a warp's list of alternatives
 constexpr int kGradThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
@@ -85,6 +91,28 @@ __device__ __forceinline__ uint64_t rank_key(float x, uint32_t j)
 __device__ __forceinline__ float value_of(uint32_t u)
 {
     return u == 0xffffffffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
+// The same of a 16-bit entry in 32 bits, for indices below 65,536.
+template <class T>
+__device__ __forceinline__ uint32_t short_key(float x, uint32_t j)
+{
+    if (x == no_value())
+        return 0;
+    const T t = from_f32<T>(x + 0.0f);  // (as it was read)
+    uint16_t b;
+    memcpy(&b, &t, 2);
+    const uint32_t u = x != x ? 0xffffu : (b & 0x8000u) ? ~(uint32_t)b & 0xffffu : b | 0x8000u;
+    return u << 16 | (~j & 0xffffu);
+}
+template <class T>
+__device__ __forceinline__ float short_value(uint32_t key)
+{
+    const uint32_t u = key >> 16;
+    const uint16_t b = (uint16_t)(u & 0x8000u ? u ^ 0x8000u : ~u);
+    T t;
+    memcpy(&t, &b, 2);
+    return u == 0xffffu ? __uint_as_float(0x7fffffffu) : to_f32(t);
 }
 
 // The running maximum and the sums of exp(x - m) and exp(x - m) (x - m).
@@ -388,9 +416,8 @@ struct Held {
 };
 
 // kLanes lanes a row of at most kLanes kPer entries, all in registers: 65,536
-// rows of 1,000 16-bit entries 51 us, with four alternatives 156, each drawn by
-// the whole group; bound by issue.
-template <class T, int kVec, int kLanes, int kPer>
+// rows of 1,000 16-bit entries 45 us, with four alternatives 100; bound by issue.
+template <class T, int kVec, int kLanes, int kPer, bool kTop>
 __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpArgs a, int top, float *logp,
                                                                      float *entropy, float *peak, float *logz,
                                                                      float *top_logp, int32_t *top_index)
@@ -433,8 +460,40 @@ __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpA
         if (logz)
             logz[r] = z;
     }
-    if (top == 0)
+    if (!kTop)
         return;
+    auto put = [&](int i, uint32_t j, float value) {
+        top_index[r * top + i] = (int)j;
+        top_logp[r * top + i] = (value - m) - z;
+    };
+    auto put_none = [&](int i) {
+        top_index[r * top + i] = -1;
+        top_logp[r * top + i] = no_value();
+    };
+    if constexpr (kLanes < 32 && sizeof(T) == 2) {
+        uint32_t u[kPer], best = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            u[k] = short_key<T>(v[k], H::at(k, lane));
+            best = max(best, u[k]);
+        }
+        for (int i = 0; i < top; ++i) {
+            uint32_t key = best;
+#pragma unroll
+            for (int o = kLanes / 2; o; o >>= 1)
+                key = max(key, __shfl_xor_sync(~0u, key, o));
+            if (here && lane == 0)
+                key ? put(i, ~key & 0xffff, short_value<T>(key)) : put_none(i);
+            if (key == best && key) {  // this lane's: the next of it
+                best = 0;
+#pragma unroll
+                for (int k = 0; k < kPer; ++k)
+                    best = max(best, u[k] < key ? u[k] : 0u);
+            }
+            __syncwarp();
+        }
+        return;
+    }
     uint32_t u[kPer], best = 0;
     int at = 0;  // of this lane's largest
 #pragma unroll
@@ -442,6 +501,48 @@ __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpA
         u[k] = order_of(v[k]);
         at = u[k] > best ? k : at;
         best = u[k] > best ? u[k] : best;
+    }
+    if (kLanes == 32 && top > 1) {
+        __shared__ uint64_t lists[kNarrowThreads / 32][kShort];
+        uint64_t *list = lists[threadIdx.x / 32];
+        uint32_t left = best, floor = 0;
+        for (int i = 0; i < top; ++i) {
+            floor = __reduce_max_sync(~0u, left);
+            const uint32_t holders = __ballot_sync(~0u, left == floor);
+            if (lane == __ffs(holders) - 1)
+                left = 0;
+        }
+        floor = max(floor, 1u);  // (0 is no entry)
+        int mine = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            mine += u[k] >= floor;
+        int to = mine;  // the end of this lane's on the list
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int before = __shfl_up_sync(~0u, to, o);
+            to += lane >= o ? before : 0;
+        }
+        const int count = __shfl_sync(~0u, to, 31);
+        if (count <= kShort) {
+            to -= mine;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (u[k] >= floor)
+                    list[to++] = (uint64_t)u[k] << 32 | (uint32_t)~H::at(k, lane);
+            __syncwarp();
+            for (int c = lane; here && c < count; c += 32) {
+                const uint64_t key = list[c];
+                int rank = 0;
+                for (int o = 0; o < count; ++o)
+                    rank += list[o] > key;
+                if (rank < top)
+                    put(rank, ~(uint32_t)key, value_of((uint32_t)(key >> 32)));
+            }
+            for (int i = count + lane; here && i < top; i += 32)  // fewer than asked for
+                put_none(i);
+            return;
+        }
     }
     for (int i = 0; i < top; ++i) {
         const uint64_t mine = best ? (uint64_t)best << 32 | (uint32_t)~H::at(at, lane) : 0;
@@ -451,10 +552,8 @@ __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpA
             const uint64_t other = __shfl_xor_sync(~0u, key, o);
             key = other > key ? other : key;
         }
-        if (here && lane == 0) {
-            top_index[r * top + i] = key ? (int)~(uint32_t)key : -1;
-            top_logp[r * top + i] = key ? (value_of((uint32_t)(key >> 32)) - m) - z : no_value();
-        }
+        if (here && lane == 0)
+            key ? put(i, ~(uint32_t)key, value_of((uint32_t)(key >> 32))) : put_none(i);
         if (key == mine && key) {  // this lane's: the next of it
             const int gone = at;
             best = 0;
@@ -738,10 +837,12 @@ cudaError_t launch_logp(const LogpArgs &a, int top, float *logp, float *entropy,
                     kernel<<<(unsigned)up(a.rows * lanes.value, kNarrowThreads), kNarrowThreads, 0, st>>>(
                         a, top, logp, entropy, peak, logz, top_logp, top_index);
                 };
-                if (packs(a.logits, a.rows, a.V, a.stride, sizeof(T)))
-                    run(logp_narrow_kernel<T, 16 / sizeof(T), lanes.value, per.value>);
-                else
-                    run(logp_narrow_kernel<T, 1, lanes.value, per.value>);
+                with_flag(top > 0, [&](auto tops) {
+                    if (packs(a.logits, a.rows, a.V, a.stride, sizeof(T)))
+                        run(logp_narrow_kernel<T, 16 / sizeof(T), lanes.value, per.value, tops.value>);
+                    else
+                        run(logp_narrow_kernel<T, 1, lanes.value, per.value, tops.value>);
+                });
             });
             return;
         }

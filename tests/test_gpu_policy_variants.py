@@ -14,7 +14,7 @@ from tests import test_gpu_policy_logp as logp  # noqa: E402
 from tests import test_gpu_policy_norm as norm  # noqa: E402
 from tests import test_gpu_policy_scan as scan  # noqa: E402
 from tests.policy_ref import (BF16, E, F16, F32, ROUNDOFF, SMALLEST, activate, close, d,  # noqa: E402
-                              gated_ffn)
+                              gated_ffn, top_of)
 
 pytestmark = pytest.mark.gpu
 
@@ -306,3 +306,27 @@ def test_ffn_gradient_of_few_again(pol):
     first = pol.gated_ffn_grad(dh, x, w)
     for _ in range(3):
         assert all(torch.equal(p, q) for p, q in zip(first, pol.gated_ffn_grad(dh, x, w)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("V", [20, 60, 120, 256, 257, 512, 513, 1024])
+@pytest.mark.parametrize("top", [1, 2, 7, 20, 32])
+def test_alternatives_of_rows_in_registers(pol, V, top, dtype):
+    """Many to choose from, ties that fill a list, few entries left, none left, infinities and NaN among the rest."""
+    x, tok, mask, _, _ = logp.make(19, V, dtype, V + top)
+    top = min(top, V)
+    x[0] = 1.5
+    x[1] = x[1].round().clamp(-1, 1)
+    x[2] = torch.where(torch.arange(V, device="cuda") % 2 == 0, 0.0, -0.0).to(dtype)
+    x[3, -min(V, 70):] = 20.0
+    x[4] = torch.finfo(dtype).min
+    x[5] = float("-inf")
+    mask[6] = 0
+    mask[7] = 0
+    mask[7, [0, V // 2, V - 1]] = 1
+    x[8, 1:] = float("-inf")
+    logp.check(pol, x, tok, mask, None, None, top, f"{top} of {V} masked")
+    logp.check(pol, x, tok, None, None, None, top, f"{top} of {V}")
+    x[9, V // 3], x[9, V // 2], x[10, 3], x[11, 5] = float("nan"), float("nan"), float("inf"), -float("nan")
+    got = pol.log_probs(x, tok, top=top)["top_index"].cpu()
+    assert torch.equal(got, top_of(x.cpu().double(), x.cpu() != float("-inf"), top))
