@@ -482,9 +482,8 @@ int av_gated_ffn(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act,
 
 /* Its gradient, dx [rows][D] and dw [2][H][D].  The projections are made
  * again, so the forward pass keeps nothing; the gradients of the two
- * projections are rounded to the arrays' type once, between the products, or
- * where rows * H <= 32768 go as two values of that type each, the second what
- * rounding the first leaves, so that only the results are rounded. */
+ * projections go to the products as two values of the arrays' type each, the
+ * second what rounding the first leaves, so that only the results are rounded. */
 int av_gated_ffn_grad(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *dh,
                       int64_t dh_stride, const void *x, int64_t x_stride, const void *w, void *dx,
                       int64_t dx_stride, void *dw, void *work, int64_t work_bytes,

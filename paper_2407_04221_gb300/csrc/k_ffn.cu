@@ -12,12 +12,10 @@
 // outputs and h leaves rounded once, with no array in between.  The backward
 // pass makes g and u again (4 M D H operations of 16) instead of keeping them:
 // kept in 16 bits they would cost accuracy, in 32 bits 8 bytes a unit.  dg and du
-// go to the last products in 16 bits, which these take: that rounding and the
-// result's own make 1.41 times the error of the latter alone, as root mean
-// square.  Where there are few of them, they need not be average, and single
-// cases reached 1.9 times (one row; 1.5 of 5 x 1,024, none from 8,192 on): there
-// (`in_two`) they go as two values, the rounded one and what it leaves, and the
-// products take both.
+// go to the last products as two values of 16 bits each, the rounded one and
+// what it leaves, and the products take both: 24 M D H operations in all, but
+// only the results are rounded.  (Rounded once in between, dx and dw were off by
+// 1.41 times as much, as root mean square.)
 //
 // Warps: one issues copies (TMA), one products, four or eight take accumulators
 // to memory while the next tile's products run (two sets of 256 TMEM columns).
@@ -45,6 +43,8 @@ __device__ __forceinline__ void activate(float g, float &f, float &slope)
     const float din = kAct == AV_SILU ? 1.0f : c * (1.0f + 3.0f * 0.044715f * g * g);
     slope = s + f * (1.0f - s) * din;
 }
+
+constexpr int kValues = 2;  // that dg and du go as: [row][value][dg, du][H]
 
 // What rounding to T leaves of v; nothing of infinity and NaN.
 template <class T>
@@ -74,7 +74,7 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float *f)
 template <class T, int kAct, int R, bool kGrad>
 __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t D, int64_t H, const T *x, int64_t xs,
                                                                const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
-                                                               T *dgu, int parts)
+                                                               T *dgu)
 {
     const int lane = threadIdx.x & 31;
     const int64_t j = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
@@ -116,14 +116,12 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t 
         if (!kGrad) {
             h[r * hs + j] = from_f32<T>(f * u[r]);
         } else {
-            const float d = to_f32(dh[r * dhs + j]);
-            T *to = dgu + r * 2 * parts * H + j;
-            to[0] = from_f32<T>(d * u[r] * slope);
-            to[H] = from_f32<T>(d * f);
-            if (parts == 2) {
-                to[2 * H] = from_f32<T>(left_of<T>(d * u[r] * slope));
-                to[3 * H] = from_f32<T>(left_of<T>(d * f));
-            }
+            const float d = to_f32(dh[r * dhs + j]), dg = d * u[r] * slope, du = d * f;
+            T *to = dgu + r * 2 * kValues * H + j;
+            to[0] = from_f32<T>(dg);
+            to[H] = from_f32<T>(du);
+            to[2 * H] = from_f32<T>(left_of<T>(dg));
+            to[3 * H] = from_f32<T>(left_of<T>(du));
         }
     }
 }
@@ -135,6 +133,7 @@ constexpr int kTile = 256;     // rows and columns of a pair's tile
 constexpr int kBlockK = 64;    // terms a stage: 128 bytes, the swizzle's width
 constexpr int kHalf = kRowsCta * kBlockK * 2;  // bytes of A or of B a CTA fetches per stage
 constexpr int kSlab = kRowsCta * 128;  // staging of 128 rows x 128 bytes on the way out
+constexpr int kHalfSlab = kSlab / 2;   // of 64 bytes
 constexpr int kTmemCols = 512;
 
 enum Form {
@@ -159,7 +158,6 @@ struct Params {
     int m_tiles, n_tiles;   // of a pair
     int k_blocks, splits;   // blocks of 64 terms in all, parts that they are dealt to
     int k_once;             // of them those of A's first value; B's come again for the second
-    int in_two;             // dg and du: 2 if they leave as two values, else 1
     const void *dh;
     int64_t dhs;
 };
@@ -273,10 +271,18 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return *reinterpret_cast<uint32_t *>(v);
 }
 
-// 16 bytes of a row into a staging slab, in the 128-byte swizzle.
+// 16 bytes of a row into a staging slab, in the 128-byte swizzle; of 64-byte
+// rows, in the 64-byte swizzle.
 __device__ __forceinline__ void put16(uint32_t slab, int row, int chunk, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     const uint32_t at = slab + row * 128 + ((chunk ^ (row & 7)) << 4);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ void put16_narrow(uint32_t slab, int row, int chunk, uint32_t a, uint32_t b, uint32_t c,
+                                             uint32_t d)
+{
+    const uint32_t at = slab + row * 64 + ((chunk ^ (row >> 1 & 3)) << 4);
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
@@ -287,6 +293,20 @@ __device__ __forceinline__ void put32(uint32_t slab, int row, int half, const fl
     for (int c = 0; c < 4; ++c)
         put16(slab, row, half * 4 + c, pack2<T>(v[8 * c], v[8 * c + 1]), pack2<T>(v[8 * c + 2], v[8 * c + 3]),
               pack2<T>(v[8 * c + 4], v[8 * c + 5]), pack2<T>(v[8 * c + 6], v[8 * c + 7]));
+}
+
+// As two values, to a half slab each.
+template <class T>
+__device__ __forceinline__ void put32_in_two(uint32_t slab, int row, const float (&v)[32])
+{
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const float *q = v + 8 * c;
+        put16_narrow(slab, row, c, pack2<T>(q[0], q[1]), pack2<T>(q[2], q[3]), pack2<T>(q[4], q[5]), pack2<T>(q[6], q[7]));
+        put16_narrow(slab + kHalfSlab, row, c, pack2<T>(left_of<T>(q[0]), left_of<T>(q[1])),
+                     pack2<T>(left_of<T>(q[2]), left_of<T>(q[3])), pack2<T>(left_of<T>(q[4]), left_of<T>(q[5])),
+                     pack2<T>(left_of<T>(q[6]), left_of<T>(q[7])));
+    }
 }
 
 __device__ __forceinline__ void team_sync(int team)
@@ -459,71 +479,69 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                         v[e] = __int_as_float(0x7fffffff);
                 }
             };
-            if (kGated) {
+            if (kForm == kForward) {
+                const int c = team * 64;  // 64 columns of H a team
+                if (first)
+                    stores_left<0>();
+                team_sync(team);
 #pragma unroll 1
-                for (int c = team * 64, part = 0; c < kRowsCta;) {  // 64 columns of H a team, each value of dg and du
+                for (int half = 0; half < 2; ++half) {
+                    float g[32], u[32];
+                    columns(c + half * 32, g);
+                    columns(kRowsCta + c + half * 32, u);
+                    wait_acc();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float f, slope;
+                        activate<kAct>(g[e], f, slope);
+                        g[e] = f * u[e];
+                    }
+                    put32<T>(slab0, row, half, g);
+                }
+                fence_async();
+                team_sync(team);
+                const int col = t.n * kRowsCta + c;
+                if (first && col < p.n && m0 < p.m)
+                    store_box(&out_map, slab0, col, 0, m0);
+                if (first)
+                    stores_close();
+            } else if (kForm == kProjGrad) {
+#pragma unroll 1
+                for (int c = team * 32; c < kRowsCta; c += 32 * kTeams) {  // 32 columns of H, both values of dg and du
                     if (first)
                         stores_left<0>();
                     team_sync(team);
-                    const uint32_t slab = slab0;
-#pragma unroll 1
-                    for (int half = 0; half < 2; ++half) {
-                        float g[32], u[32];
-                        columns(c + half * 32, g);
-                        columns(kRowsCta + c + half * 32, u);
-                        const int col = t.n * kRowsCta + c + half * 32;
-                        if (kForm == kForward) {
-                            wait_acc();
+                    const int col = t.n * kRowsCta + c;
+                    float g[32], u[32], d[32];
+                    columns(c, g);
+                    columns(kRowsCta + c, u);
+                    const T *dh = (const T *)p.dh + (int64_t)(m0 + row) * p.dhs + col;
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                float f, slope;
-                                activate<kAct>(g[e], f, slope);
-                                g[e] = f * u[e];
-                            }
-                            put32<T>(slab, row, half, g);
-                        } else {
-                            const T *dh = (const T *)p.dh + (int64_t)(m0 + row) * p.dhs + col;
-                            float d[32];
-#pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
-                                uint4 q = make_uint4(0, 0, 0, 0);
-                                if (m0 + row < p.m && col + e < p.n)
-                                    q = __ldg(reinterpret_cast<const uint4 *>(dh + e));
-                                unpack8<T>(q, d + e);
-                            }
-                            wait_acc();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                float f, slope;
-                                activate<kAct>(g[e], f, slope);
-                                g[e] = d[e] * u[e] * slope;
-                                u[e] = d[e] * f;
-                            }
-                            if (part) {
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    g[e] = left_of<T>(g[e]);
-                                    u[e] = left_of<T>(u[e]);
-                                }
-                            }
-                            put32<T>(slab, row, half, g);
-                            put32<T>(slab + kSlab, row, half, u);
-                        }
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 q = make_uint4(0, 0, 0, 0);
+                        if (m0 + row < p.m && col + e < p.n)
+                            q = __ldg(reinterpret_cast<const uint4 *>(dh + e));
+                        unpack8<T>(q, d + e);
                     }
+                    wait_acc();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float f, slope;
+                        activate<kAct>(g[e], f, slope);
+                        g[e] = d[e] * u[e] * slope;
+                        u[e] = d[e] * f;
+                    }
+                    put32_in_two<T>(slab0, row, g);
+                    put32_in_two<T>(slab0 + kSlab, row, u);
                     fence_async();
                     team_sync(team);
-                    if (first && t.n * kRowsCta + c < p.n && m0 < p.m) {
-                        const int col = t.n * kRowsCta + c;
-                        store_box(&out_map, slab, col, 2 * part, m0);
-                        if (kForm == kProjGrad)
-                            store_box(&out_map, slab + kSlab, col, 2 * part + 1, m0);
+                    if (first && col < p.n && m0 < p.m) {
+#pragma unroll
+                        for (int k = 0; k < 2 * kValues; ++k)  // dg, du, and what they left
+                            store_box(&out_map, slab0 + (k & 1) * kSlab + (k >> 1) * kHalfSlab, col, k, m0);
                     }
                     if (first)
                         stores_close();
-                    if (kForm == kForward || ++part == p.in_two) {
-                        part = 0;
-                        c += 64 * kTeams;
-                    }
                 }
             } else {
                 constexpr int kWide = kParts ? 32 : 64;  // columns of 128 bytes
@@ -604,9 +622,9 @@ bool operand_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64
 }
 
 // dg and du as A: [value][row][2 H] by columns, rows and values, boxes of box_rows x 64 columns.
-bool grads_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64_t H, int parts, int box_rows)
+bool grads_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64_t H, int box_rows)
 {
-    const int64_t dims[3] = {2 * H, rows, parts}, strides[2] = {2 * parts * H, 2 * H};
+    const int64_t dims[3] = {2 * H, rows, kValues}, strides[2] = {2 * kValues * H, 2 * H};
     const int box[3] = {64, box_rows, 1};
     return make_map(map, dtype, p, 3, dims, strides, box);
 }
@@ -614,14 +632,6 @@ bool grads_map(CUtensorMap *map, int dtype, const void *p, int64_t rows, int64_t
 constexpr int kPairs = 76;  // of a GB300's 152 SMs
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// Values that dg and du go as: two where there are up to 32,768 of either, some
-// six times what the largest case of more than 1.5 times the error had (5 x
-// 1,024).  There it costs little: 4 x 1,024 x 4,096 38 us once and 40 twice, 16 x
-// 1,024 x 1,024 32 and 37; 16,384 x 1,024 x 4,096 would take half as long again.
-int in_two(int64_t rows, int64_t H) { return rows * H <= 32768 ? 2 : 1; }
-
-int64_t blocks_of(int64_t k, int parts) { return up(k, kBlockK) * parts; }
 
 // Into how many parts the terms of a product are dealt: the number that ends
 // soonest.  A block of 64 terms takes a pair 0.27 us; each part writes its
@@ -651,7 +661,7 @@ int64_t parts_bytes(int64_t m, int64_t n, int64_t blocks)
     return s > 1 ? (int64_t)s * m * n * 4 : 0;
 }
 
-int64_t dgu_bytes(int64_t rows, int64_t H) { return up(rows * 2 * H * 2 * in_two(rows, H), 256) * 256; }
+int64_t dgu_bytes(int64_t rows, int64_t H) { return up(rows * 2 * kValues * H * 2, 256) * 256; }
 
 template <class T, int kForm, int kAct, bool kParts>
 cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Params &p, cudaStream_t st,
@@ -666,10 +676,10 @@ cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &ou
                           chained, a, b, out, p);
 }
 
-// out [m][n] = A B, in one go or in parts.
+// out [m][n] = A B, A as two values, in one go or in parts.
 template <class T, int kForm>
 cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64_t m, int64_t n, int64_t k, void *out,
-                    int64_t os, float *parts, int values, cudaStream_t st)
+                    int64_t os, float *parts, cudaStream_t st)
 {
     Params p{};
     p.m = (int)m;
@@ -677,7 +687,7 @@ cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64
     p.m_tiles = (int)up(m, kTile);
     p.n_tiles = (int)up(n, kTile);
     p.k_once = (int)up(k, kBlockK);
-    p.k_blocks = (int)blocks_of(k, values);
+    p.k_blocks = kValues * p.k_once;
     p.splits = splits_for(m, n, p.k_blocks);
     CUtensorMap map;
     const int64_t dims[3] = {n, m, p.splits};
@@ -702,23 +712,23 @@ cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64
 
 template <class T, int kAct, bool kGrad>
 void few(int rows, int64_t D, int64_t H, const T *x, int64_t xs, const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
-         T *dgu, int parts, cudaStream_t st)
+         T *dgu, cudaStream_t st)
 {
     const unsigned grid = (unsigned)up(H, kFewThreads / 32);
     if (rows <= 1)
-        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu, parts);
+        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
     else
-        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu, parts);
+        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
 }
 
-// h, or the projections' gradients [rows][2][H].
+// h, or the projections' gradients [rows][value][2][H].
 template <class T, int kAct, bool kGrad>
 cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, int64_t xs, const void *w, void *h,
                   int64_t hs, const void *dh, int64_t dhs, void *dgu, cudaStream_t st)
 {
     if (rows <= kFewRows) {
         few<T, kAct, kGrad>((int)rows, D, H, (const T *)x, xs, (const T *)w, (T *)h, hs, (const T *)dh, dhs, (T *)dgu,
-                            in_two(rows, H), st);
+                            st);
         return cudaGetLastError();
     }
     Params p{};
@@ -729,15 +739,14 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
     p.k_blocks = (int)up(D, kBlockK);
     p.k_once = p.k_blocks;
     p.splits = 1;
-    p.in_two = in_two(rows, H);
     p.dh = dh;
     p.dhs = dhs;
     CUtensorMap a, b, out;
     // (stores are columns, projection of a value, row; h has one)
-    const int64_t dims[3] = {H, kGrad ? 2 * p.in_two : 1, rows}, strides[2] = {H, kGrad ? 2 * p.in_two * H : hs};
-    const int box[3] = {64, 1, kRowsCta};
+    const int64_t dims[3] = {H, kGrad ? 2 * kValues : 1, rows}, strides[2] = {H, kGrad ? 2 * kValues * H : hs};
+    const int box[3] = {kGrad ? 32 : 64, 1, kRowsCta};
     if (!operand_map(&a, dtype, x, rows, D, xs, kRowsCta) || !operand_map(&b, dtype, w, 2 * H, D, D, kRowsCta) ||
-        !make_map(&out, dtype, kGrad ? dgu : h, 3, dims, strides, box))
+        !make_map(&out, dtype, kGrad ? dgu : h, 3, dims, strides, box, kGrad ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
     return go<T, kGrad ? kProjGrad : kForward, kAct, false>(a, b, out, p, st, false);
 }
@@ -746,8 +755,8 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
 
 int64_t ffn_work_bytes(int64_t rows, int64_t D, int64_t H)
 {
-    const int64_t a = parts_bytes(rows, D, blocks_of(2 * H, in_two(rows, H))),
-                  b = parts_bytes(2 * H, D, blocks_of(rows, in_two(rows, H)));
+    const int64_t a = parts_bytes(rows, D, kValues * up(2 * H, kBlockK)),
+                  b = parts_bytes(2 * H, D, kValues * up(rows, kBlockK));
     return dgu_bytes(rows, H) + (a > b ? a : b);
 }
 
@@ -782,14 +791,13 @@ cudaError_t launch_ffn_grad(int64_t rows, int64_t D, int64_t H, int dtype, int a
         if (e != cudaSuccess)
             return e;
         CUtensorMap dgu, wt, dgut, xt;
-        const int values = in_two(rows, H);
-        if (!grads_map(&dgu, dtype, work, rows, H, values, kRowsCta) || !operand_map(&wt, dtype, w, 2 * H, D, D, 64) ||
-            !grads_map(&dgut, dtype, work, rows, H, values, 64) || !operand_map(&xt, dtype, x, rows, D, x_stride, 64))
+        if (!grads_map(&dgu, dtype, work, rows, H, kRowsCta) || !operand_map(&wt, dtype, w, 2 * H, D, D, 64) ||
+            !grads_map(&dgut, dtype, work, rows, H, 64) || !operand_map(&xt, dtype, x, rows, D, x_stride, 64))
             return cudaErrorInvalidValue;
-        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, values, st);
+        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, st);
         if (e != cudaSuccess)
             return e;
-        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, values, st);
+        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, st);
     };
     return dtype == AV_BF16 ? run(__nv_bfloat16()) : run(__half());
 }

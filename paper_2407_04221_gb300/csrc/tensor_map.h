@@ -29,9 +29,9 @@ inline EncodeTiled map_encoder()
 }
 
 // dims, box: innermost first; strides of the outer dims, in elements.  Boxes
-// are 128 bytes wide, in the 128-byte swizzle.
+// are as wide as the swizzle: 128 bytes, or 64.
 inline bool make_map(CUtensorMap *map, int dtype, const void *p, int rank, const int64_t *dims, const int64_t *strides,
-                     const int *box)
+                     const int *box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
     const int64_t e = dtype == AV_F32 ? 4 : 2;
     cuuint64_t d[5], s[4];
@@ -47,7 +47,7 @@ inline bool make_map(CUtensorMap *map, int dtype, const void *p, int rank, const
                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     const EncodeTiled encode = map_encoder();
     return encode && encode(map, type, (cuuint32_t)rank, const_cast<void *>(p), d, s, b, one,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
