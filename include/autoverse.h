@@ -483,7 +483,10 @@ int av_gated_ffn(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act,
 /* Its gradient, dx [rows][D] and dw [2][H][D].  The projections are made
  * again, so the forward pass keeps nothing; the gradients of the two
  * projections go to the products as two values of the arrays' type each, the
- * second what rounding the first leaves, so that only the results are rounded. */
+ * second what rounding the first leaves, so that only the results are rounded.
+ * Of AV_F16 they go times a power of two that keeps the largest in range: a
+ * result is infinite where it is itself beyond the type, and values down to
+ * 2^-36 of the largest gradient of a projection count. */
 int av_gated_ffn_grad(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *dh,
                       int64_t dh_stride, const void *x, int64_t x_stride, const void *w, void *dx,
                       int64_t dx_stride, void *dw, void *work, int64_t work_bytes,

@@ -15,7 +15,9 @@
 // go to the last products as two values of 16 bits each, the rounded one and
 // what it leaves, and the products take both: 24 M D H operations in all, but
 // only the results are rounded.  (Rounded once in between, dx and dw were off by
-// 1.41 times as much, as root mean square.)
+// 1.41 times as much, as root mean square.)  float16 has not the range for them:
+// they go times a power of two, which a bound on their largest gives
+// (`ffn_peaks_kernel`), and the results are brought back before they are rounded.
 //
 // Warps: one issues copies (TMA), one products, four or eight take accumulators
 // to memory while the next tile's products run (two sets of 256 TMEM columns).
@@ -54,10 +56,7 @@ __device__ __forceinline__ float left_of(float v)
     return fabsf(r) <= 3.402823466e38f ? v - r : 0.0f;
 }
 
-// ------------------------------------------------------------ few rows
-
-constexpr int kFewRows = 4;  // (eight: 18.6 us, 16: 28.8, by tensor cores 12.5, at 1,024 x 4,096)
-constexpr int kFewThreads = 256;
+// ------------------------------------------------------------ float16's range
 
 template <class T>
 __device__ __forceinline__ void unpack8(const uint4 &v, float *f)
@@ -68,13 +67,94 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float *f)
         f[i] = to_f32(p[i]);
 }
 
+template <class T>
+constexpr bool kScaled = std::is_same<T, __half>::value;
+constexpr int kPeakThreads = 256;
+
+// What bounds dg and du: the largest |dh|, and the largest sums of squares of a
+// row of x and of w; each in 32 places, of which the largest counts.
+using Peaks = const float4 *;
+constexpr int kPeakBytes = 32 * 16;
+
+// A power of two that brings dg and du below 2^15: |dg| <= |dh| |u| 1.13 and |du|
+// <= |dh| |g|, projections are no larger than the product of their rows'
+// lengths.  The bound is some ten times the largest value, so this is good to
+// 2^-22 and, of the smallest, 2^-36 of the largest.  For whole warps.
+__device__ __forceinline__ float scale_of(Peaks p)
+{
+    float4 v = p[threadIdx.x & 31];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        v.x = fmaxf(v.x, __shfl_xor_sync(~0u, v.x, o));
+        v.y = fmaxf(v.y, __shfl_xor_sync(~0u, v.y, o));
+        v.z = fmaxf(v.z, __shfl_xor_sync(~0u, v.z, o));
+    }
+    const float most = 1.16f * v.x * sqrtf(v.y) * sqrtf(v.z);
+    if (!(most > 0.0f))
+        return 1.0f;
+    const int k = 15 - ((int)(__float_as_uint(most) >> 23) - 126);  // (most < 2^(exponent - 126))
+    return __int_as_float((127 + min(max(k, -60), 60)) << 23);
+}
+
+// The peaks, of finite values; they are zeroed before.  A warp takes a row, of dh,
+// x or w by the block's y; maxima do not depend on their order.  4,099 x 520 x
+// 1,368 7 us, 65,536 x 256 x 512 21, both from memory.
+template <class T>
+__global__ __launch_bounds__(kPeakThreads) void ffn_peaks_kernel(int64_t rows, int64_t D, int64_t H, const T *x, int64_t xs,
+                                                                 const T *w, const T *dh, int64_t dhs, float4 *peaks)
+{
+    constexpr int kWarps = kPeakThreads / 32;
+    __shared__ float of_warps[kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
+    const T *from = which == 0 ? dh : which == 1 ? x : w;
+    const int64_t n = which == 0 ? H : D, count = which == 2 ? 2 * H : rows, stride = which == 0 ? dhs : which == 1 ? xs : D;
+    float most = 0.0f;
+    for (int64_t r = (int64_t)blockIdx.x * kWarps + warp; r < count; r += (int64_t)gridDim.x * kWarps) {
+        const T *row = from + r * stride;
+        float sum = 0.0f, top = 0.0f;
+#pragma unroll 8
+        for (int64_t k = lane * 8; k < n; k += 256) {
+            float v[8];
+            unpack8<T>(__ldg(reinterpret_cast<const uint4 *>(row + k)), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float a = fabsf(v[e]) <= 3.402823466e38f ? fabsf(v[e]) : 0.0f;
+                sum = fmaf(a, a, sum);
+                top = fmaxf(top, a);
+            }
+        }
+        if (which != 0) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1)
+                sum += __shfl_xor_sync(~0u, sum, o);
+        }
+        most = fmaxf(most, which == 0 ? top : sum);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+        most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    if (lane == 0)
+        of_warps[warp] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < kWarps; ++k)
+            most = fmaxf(most, of_warps[k]);
+        atomicMax(reinterpret_cast<int *>(peaks + (blockIdx.x & 31)) + which, __float_as_int(most));  // (none is negative)
+    }
+}
+
+// ------------------------------------------------------------ few rows
+
+constexpr int kFewRows = 4;  // (eight: 18.6 us, 16: 28.8, by tensor cores 12.5, at 1,024 x 4,096)
+constexpr int kFewThreads = 256;
+
 // A warp per unit of H: its two rows of weights stream past, 16 bytes a lane,
 // against R rows of x that stay in L1.  Bound by the weights' bytes: 4 x 1,024 x
 // 4,096 8.2 us, 2.0 TB/s, of which some 3 are the launch.
 template <class T, int kAct, int R, bool kGrad>
 __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t D, int64_t H, const T *x, int64_t xs,
                                                                const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
-                                                               T *dgu)
+                                                               T *dgu, Peaks peaks)
 {
     const int lane = threadIdx.x & 31;
     const int64_t j = (int64_t)blockIdx.x * (kFewThreads / 32) + (threadIdx.x >> 5);
@@ -83,6 +163,7 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t 
     if (j >= H)
         return;
     const T *wg = w + j * D, *wu = w + (H + j) * D;
+    const float scale = kGrad && kScaled<T> ? scale_of(peaks) : 1.0f;
     float g[R] = {}, u[R] = {};
 #pragma unroll 2
     for (int64_t k = lane * 8; k < D; k += 256) {
@@ -116,7 +197,7 @@ __global__ __launch_bounds__(kFewThreads) void ffn_few_kernel(int rows, int64_t 
         if (!kGrad) {
             h[r * hs + j] = from_f32<T>(f * u[r]);
         } else {
-            const float d = to_f32(dh[r * dhs + j]), dg = d * u[r] * slope, du = d * f;
+            const float d = to_f32(dh[r * dhs + j]) * scale, dg = d * u[r] * slope, du = d * f;
             T *to = dgu + r * 2 * kValues * H + j;
             to[0] = from_f32<T>(dg);
             to[H] = from_f32<T>(du);
@@ -160,6 +241,7 @@ struct Params {
     int k_once;             // of them those of A's first value; B's come again for the second
     const void *dh;
     int64_t dhs;
+    Peaks peaks;            // what dg and du are scaled by, of float16
 };
 
 __device__ __forceinline__ uint32_t cta_rank()
@@ -461,6 +543,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
         const int team = (warp - 2) >> 2;
         const bool first = (threadIdx.x - 64) % 128 == 0;  // issues its team's stores
         const uint32_t slab0 = slabs + team * kSlabs * kSlab;
+        const float scale = kScaled<T> && kForm != kForward ? scale_of(p.peaks) : 1.0f, back = 1.0f / scale;
         int done = 0;
         for (int i = pair; i < tiles; i += pairs, ++done) {
             const Tile t = tile_of(p, i);
@@ -528,8 +611,9 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     for (int e = 0; e < 32; ++e) {
                         float f, slope;
                         activate<kAct>(g[e], f, slope);
-                        g[e] = d[e] * u[e] * slope;
-                        u[e] = d[e] * f;
+                        const float up = kScaled<T> ? d[e] * scale : d[e];
+                        g[e] = up * u[e] * slope;
+                        u[e] = up * f;
                     }
                     put32_in_two<T>(slab0, row, g);
                     put32_in_two<T>(slab0 + kSlab, row, u);
@@ -564,6 +648,11 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                         for (int half = 0; half < 2; ++half) {
                             columns(c + half * 32, v);
                             wait_acc();
+                            if (kScaled<T>) {
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    v[e] *= back;
+                            }
                             put32<T>(slab, row, half, v);
                         }
                     }
@@ -594,19 +683,23 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
 }
 
-// The sum of the parts, rounded; parts in order.
+// The sum of the parts, brought back from its scale and rounded; parts in order.
 template <class T>
-__global__ void ffn_parts_kernel(int64_t rows, int64_t cols, int splits, const float *parts, T *out, int64_t os)
+__global__ void ffn_parts_kernel(int64_t rows, int64_t cols, int splits, const float *parts, T *out, int64_t os,
+                                 Peaks peaks)
 {
     const int64_t per = cols / 4, n = rows * per;
     next_may_start();
     after_previous();
+    const float back = kScaled<T> ? 1.0f / scale_of(peaks) : 1.0f;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
         float4 v = reinterpret_cast<const float4 *>(parts)[i];
         for (int s = 1; s < splits; ++s) {
             const float4 q = reinterpret_cast<const float4 *>(parts)[i + s * n];
             v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
         }
+        if (kScaled<T>)
+            v.x *= back, v.y *= back, v.z *= back, v.w *= back;
         *reinterpret_cast<uint2 *>(out + i / per * os + i % per * 4) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
     }
 }
@@ -679,9 +772,10 @@ cudaError_t go(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &ou
 // out [m][n] = A B, A as two values, in one go or in parts.
 template <class T, int kForm>
 cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64_t m, int64_t n, int64_t k, void *out,
-                    int64_t os, float *parts, cudaStream_t st)
+                    int64_t os, float *parts, Peaks peaks, cudaStream_t st)
 {
     Params p{};
+    p.peaks = peaks;
     p.m = (int)m;
     p.n = (int)n;
     p.m_tiles = (int)up(m, kTile);
@@ -707,28 +801,28 @@ cudaError_t product(int dtype, const CUtensorMap &a, const CUtensorMap &b, int64
         return e;
     const int64_t blocks = up(m * n / 4, 256);
     return launch_chained(ffn_parts_kernel<T>, (unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 256, 0, st, true, m, n,
-                          p.splits, parts, (T *)out, m > 1 ? os : n);
+                          p.splits, parts, (T *)out, m > 1 ? os : n, peaks);
 }
 
 template <class T, int kAct, bool kGrad>
 void few(int rows, int64_t D, int64_t H, const T *x, int64_t xs, const T *w, T *h, int64_t hs, const T *dh, int64_t dhs,
-         T *dgu, cudaStream_t st)
+         T *dgu, Peaks peaks, cudaStream_t st)
 {
     const unsigned grid = (unsigned)up(H, kFewThreads / 32);
     if (rows <= 1)
-        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+        ffn_few_kernel<T, kAct, 1, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu, peaks);
     else
-        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu);
+        ffn_few_kernel<T, kAct, kFewRows, kGrad><<<grid, kFewThreads, 0, st>>>(rows, D, H, x, xs, w, h, hs, dh, dhs, dgu, peaks);
 }
 
 // h, or the projections' gradients [rows][value][2][H].
 template <class T, int kAct, bool kGrad>
 cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, int64_t xs, const void *w, void *h,
-                  int64_t hs, const void *dh, int64_t dhs, void *dgu, cudaStream_t st)
+                  int64_t hs, const void *dh, int64_t dhs, void *dgu, Peaks peaks, cudaStream_t st)
 {
     if (rows <= kFewRows) {
         few<T, kAct, kGrad>((int)rows, D, H, (const T *)x, xs, (const T *)w, (T *)h, hs, (const T *)dh, dhs, (T *)dgu,
-                            st);
+                            peaks, st);
         return cudaGetLastError();
     }
     Params p{};
@@ -741,6 +835,7 @@ cudaError_t gated(int dtype, int64_t rows, int64_t D, int64_t H, const void *x, 
     p.splits = 1;
     p.dh = dh;
     p.dhs = dhs;
+    p.peaks = peaks;
     CUtensorMap a, b, out;
     // (stores are columns, projection of a value, row; h has one)
     const int64_t dims[3] = {H, kGrad ? 2 * kValues : 1, rows}, strides[2] = {H, kGrad ? 2 * kValues * H : hs};
@@ -757,7 +852,7 @@ int64_t ffn_work_bytes(int64_t rows, int64_t D, int64_t H)
 {
     const int64_t a = parts_bytes(rows, D, kValues * up(2 * H, kBlockK)),
                   b = parts_bytes(2 * H, D, kValues * up(rows, kBlockK));
-    return dgu_bytes(rows, H) + (a > b ? a : b);
+    return dgu_bytes(rows, H) + (a > b ? a : b) + kPeakBytes;  // (the peaks last)
 }
 
 cudaError_t launch_ffn(int64_t rows, int64_t D, int64_t H, int dtype, int act, const void *x, int64_t x_stride,
@@ -768,9 +863,9 @@ cudaError_t launch_ffn(int64_t rows, int64_t D, int64_t H, int dtype, int act, c
     auto run = [&](auto v) {
         using T = decltype(v);
         return act == AV_SILU ? gated<T, AV_SILU, false>(dtype, rows, D, H, x, x_stride, w, h, h_stride, nullptr, 0,
-                                                         nullptr, st)
+                                                         nullptr, nullptr, st)
                               : gated<T, AV_GELU, false>(dtype, rows, D, H, x, x_stride, w, h, h_stride, nullptr, 0,
-                                                         nullptr, st);
+                                                         nullptr, nullptr, st);
     };
     return dtype == AV_BF16 ? run(__nv_bfloat16()) : run(__half());
 }
@@ -782,22 +877,32 @@ cudaError_t launch_ffn_grad(int64_t rows, int64_t D, int64_t H, int dtype, int a
     if (!map_encoder())
         return cudaErrorNotSupported;
     float *parts = reinterpret_cast<float *>((char *)work + dgu_bytes(rows, H));
+    float4 *peaks = reinterpret_cast<float4 *>((char *)work + ffn_work_bytes(rows, D, H) - kPeakBytes);
     auto run = [&](auto v) {
         using T = decltype(v);
-        cudaError_t e = act == AV_SILU ? gated<T, AV_SILU, true>(dtype, rows, D, H, x, x_stride, w, nullptr, 0, dh,
-                                                                 dh_stride, work, st)
+        cudaError_t e = cudaSuccess;
+        if constexpr (kScaled<T>) {
+            e = cudaMemsetAsync(peaks, 0, kPeakBytes, st);
+            if (e != cudaSuccess)
+                return e;
+            const int64_t blocks = up(rows > 2 * H ? rows : 2 * H, kPeakThreads / 32);
+            ffn_peaks_kernel<T><<<dim3((unsigned)(blocks < 152 * 8 ? blocks : 152 * 8), 3), kPeakThreads, 0, st>>>(
+                rows, D, H, (const T *)x, x_stride, (const T *)w, (const T *)dh, dh_stride, peaks);
+        }
+        e = act == AV_SILU ? gated<T, AV_SILU, true>(dtype, rows, D, H, x, x_stride, w, nullptr, 0, dh,
+                                                                 dh_stride, work, peaks, st)
                                        : gated<T, AV_GELU, true>(dtype, rows, D, H, x, x_stride, w, nullptr, 0, dh,
-                                                                 dh_stride, work, st);
+                                                                 dh_stride, work, peaks, st);
         if (e != cudaSuccess)
             return e;
         CUtensorMap dgu, wt, dgut, xt;
         if (!grads_map(&dgu, dtype, work, rows, H, kRowsCta) || !operand_map(&wt, dtype, w, 2 * H, D, D, 64) ||
             !grads_map(&dgut, dtype, work, rows, H, 64) || !operand_map(&xt, dtype, x, rows, D, x_stride, 64))
             return cudaErrorInvalidValue;
-        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, st);
+        e = product<T, kTimesW>(dtype, dgu, wt, rows, D, 2 * H, dx, dx_stride, parts, peaks, st);
         if (e != cudaSuccess)
             return e;
-        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, st);
+        return product<T, kTransposed>(dtype, dgut, xt, 2 * H, D, rows, dw, D, parts, peaks, st);
     };
     return dtype == AV_BF16 ? run(__nv_bfloat16()) : run(__half());
 }

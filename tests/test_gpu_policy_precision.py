@@ -41,3 +41,22 @@ def rounded_once(pol, x, w, dh, act, what):
 @pytest.mark.parametrize("rows,D,H", [(4, 136, 8200), (129, 256, 256), (300, 520, 136), (1025, 64, 72), (3000, 264, 520)])
 def test_ffn_gradient_is_as_exact_as_rounding_once(pol, rows, D, H, dtype, act):
     rounded_once(pol, *ffn.make(rows, D, H, dtype, rows + H), act, f"{rows} {D} {H} {dtype}")
+
+
+@pytest.mark.parametrize("rows", [3, 20, 150])
+def test_ffn_gradient_of_large_values(pol, rows):
+    """float16: gradients of the projections far beyond 65,504, of which the results are finite."""
+    x, w, dh = ffn.make(rows, 64, 72, F16, rows)
+    x, dh = x * 2.0**-7, (dh.float().clamp(-2, 2) * 30000).half()
+    w = torch.stack((w[0] * 2.0**-7, w[1] * 512))
+    g = d(dh) * (d(x) @ d(w[1]).t())
+    assert float(g.abs().max()) > 4 * 65504
+    rounded_once(pol, x, w, dh, "silu", f"{rows}")
+
+
+@pytest.mark.parametrize("rows", [2, 500, 3000])
+def test_ffn_gradient_of_small_values(pol, rows):
+    """float16: gradients of the projections near the smallest values, of which the results are sums of many or large
+    multiples."""
+    x, w, dh = ffn.make(rows, 64, 520, F16, rows)
+    rounded_once(pol, x * 64, w * 2.0**-4, (dh.float() * 2.0**-18).half(), "gelu", f"{rows}")
