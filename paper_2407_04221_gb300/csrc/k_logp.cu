@@ -625,7 +625,7 @@ __global__ __launch_bounds__(kTinyThreads) void logp_tiny_kernel(const LogpArgs 
     }
 }
 
-// What a row's gradient takes; c and de 2^-24 of what they are.
+// What a row's gradient takes; c is dl + de entropy.
 struct Slope {
     float m, z, dl, c, de;
     int64_t tok;
@@ -641,19 +641,24 @@ __device__ __forceinline__ Slope slope_of(const LogpArgs &a, int64_t r, const fl
     s.de = dentropy ? dentropy[r] : 0.0f;
     s.tok = token_of(a.tokens, a.token_bytes, r);
     s.dl = dlogp && s.tok >= 0 && s.tok < a.V ? dlogp[r] : 0.0f;
-    s.c = (s.dl + s.de * (dentropy ? entropy[r] : 0.0f)) * 0x1p-24f;
-    s.de *= 0x1p-24f;
+    s.c = s.dl + s.de * (dentropy ? entropy[r] : 0.0f);
     return s;
 }
 
-// Of an entry (-inf where it is masked), but for the token's own dlogp.  The
-// exponential is taken 2^24 times too large: it flushes to 0 at 2^-126, where
-// its product with a log probability does not yet.
+// exp2 with its smallest values: of 2^-126 and below the product with a log
+// probability is not yet so small.
+__device__ __forceinline__ float exp2_whole(float v)
+{
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// Of an entry (-inf where it is masked), but for the token's own dlogp.
 __device__ __forceinline__ float slope_at(const Slope &s, float x)
 {
     const float lp = max_nan((x - s.m) - s.z, -200.0f);
-    const float p = exp2_fast(fmaf(lp, kLog2e, 24.0f));
-    return -p * fmaf(s.de, lp, s.c);
+    return -exp2_whole(lp * kLog2e) * fmaf(s.de, lp, s.c);
 }
 
 // An entry's gradient whole.

@@ -7,7 +7,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests import test_gpu_policy_ffn as ffn  # noqa: E402
-from tests.policy_ref import BF16, F16, d, gated_ffn  # noqa: E402
+from tests import test_gpu_policy_logp as logp  # noqa: E402
+from tests.policy_ref import BF16, F16, F32, close, d, gated_ffn  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +61,27 @@ def test_ffn_gradient_of_small_values(pol, rows):
     multiples."""
     x, w, dh = ffn.make(rows, 64, 520, F16, rows)
     rounded_once(pol, x * 64, w * 2.0**-4, (dh.float() * 2.0**-18).half(), "gelu", f"{rows}")
+
+
+# ------------------------------------------------------------ log probabilities
+
+@pytest.mark.parametrize("rows,V", [(20000, 2), (20000, 5), (20000, 8), (5000, 20), (2000, 64), (500, 1000), (300, 3000),
+                                    (1300, 3000), (3, 50000)])
+@pytest.mark.parametrize("sure", [False, True])
+def test_gradient_of_32_bit_logits(pol, rows, V, sure):
+    """Against the formula of what the forward pass returned, in 64 bits.  With e = 2^-24: log p = (x - peak) - logz is
+    off by e (|x - peak| + |log p|); its product with log2(e), itself rounded, by 2 e |log p| more; the exponential by
+    2^-22 relatively: p by e (|x - peak| + 3 |log p| + 4).  c = dlogp + dentropy entropy is off by e (|c| + |dentropy
+    entropy|), dentropy log p + c by e of itself and dentropy times log p's error more, their product with p by e."""
+    x, tok, _, dl, de = logp.make(rows, V, F32, rows + V)
+    if sure:  # of the token: p near one
+        x[torch.arange(rows), tok] = x.amax(1) + 6 + 10 * torch.rand(rows, generator=torch.Generator().manual_seed(V)).cuda()
+    out = pol.log_probs(x, tok)
+    got = pol.log_probs_grad(dl, de, x, tok, out)
+    low = d(x) - d(out["peak"])[:, None]
+    lp, dl, de, H = low - d(out["logz"])[:, None], d(dl)[:, None], d(de)[:, None], d(out["entropy"])[:, None]
+    p, c = lp.exp(), dl + de * H
+    q = c + de * lp
+    want = dl * (torch.arange(V) == tok.cpu()[:, None]) - p * q
+    scale = p * (q.abs() * (low.abs() + 3 * lp.abs() + 6) + c.abs() + (de * H).abs() + de.abs() * (low.abs() + lp.abs()))
+    close(got, want, 1.02 * scale, f"{rows}x{V}")
