@@ -362,12 +362,13 @@ __global__ __launch_bounds__(kWideThreads) void logp_wide_kernel(const LogpArgs 
                 top_logp[r * top + k] = no_value();
             }
         } else {
-            uint64_t last = ~0ull;
+            uint64_t last = 0;
             for (int k = 0; k < top; ++k) {
                 uint64_t best = 0;
+                // (the first of all may have any key: of NaN at index 0 all bits are set)
                 entries<kWideThreads, kMask>(row, thread, 0, 1, [&](float v, int j) {
                     const uint64_t key = rank_key(v, j);
-                    best = key < last && key > best ? key : best;
+                    best = (k == 0 || key < last) && key > best ? key : best;
                 });
 #pragma unroll
                 for (int o = 16; o; o >>= 1) {
