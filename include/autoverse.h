@@ -426,7 +426,7 @@ int av_scan(int64_t T, int64_t B, int64_t D, int32_t dtype, const void *gate, in
 /* Its gradient, from dh (of h) and dlast (float [B][D], of h_last, or NULL):
  *   l_t = dh_t + a_{t+1} k_{t+1} l_{t+1}, dlast added to l_{T-1},
  *   dvalue_t = (1 - a_t) l_t,  dgate_t = l_t (k_t h_{t-1} - value_t) a_t (1 - a_t),
- *   dh0 = a_0 k_0 l_0  (float [B][D], or NULL).
+ *   dh0 = a_0 k_0 l_0  (float [B][D], or NULL; it may be dlast itself).
  * gate, value, reset are av_scan's and states what it kept. */
 int av_scan_grad(int64_t T, int64_t B, int64_t D, int32_t dtype, const void *dh, int64_t dh_t,
                  int64_t dh_b, const void *gate, int64_t gate_t, int64_t gate_b, const void *value,

@@ -897,10 +897,11 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
                 run.states(tile, h);
             carry[0] = apply(total.A[0], total.H[0], carry[0]);
             carry[1] = apply(total.A[1], total.H[1], carry[1]);
-            if (a.last && item.place == a.chunks - 1 && speaks) {
-                if (c.first)
+            if (a.last && item.place == a.chunks - 1) {
+                __syncwarp();  // (all lanes have read what entered, which may lie there)
+                if (speaks && c.first)
                     a.last[item.c + channel] = carry[0];
-                if (c.second)
+                if (speaks && c.second)
                     a.last[item.c + channel + 1] = carry[1];
             }
             const bool out_tma = by_tma(item);
@@ -1147,6 +1148,10 @@ int64_t segments_of(int64_t slabs, int64_t chunks, int64_t resident)
 
 int64_t resident_of(int e, bool back, int run) { return (int64_t)kSms * blocks_of(e, back, run); }
 
+// The segments' maps, and [B D] floats for the states that enter the sequences
+// where those that leave take their place.
+int64_t map_bytes(int64_t slabs, int64_t segments) { return slabs * segments * kMaps * (int64_t)sizeof(Map2); }
+
 int64_t work_bytes(int64_t T, int64_t B, int64_t D, int e)
 {
     int64_t most = 0;
@@ -1154,7 +1159,7 @@ int64_t work_bytes(int64_t T, int64_t B, int64_t D, int e)
         for (int back = 0; back < 2; ++back) {
             const int64_t slabs = slabs_of(B, D, flat),
                           n = segments_of(slabs, chunks_of(T, e), resident_of(e, back, run_of(T, e)));
-            const int64_t need = n > 1 ? slabs * n * kMaps * (int64_t)sizeof(Map2) : 0;
+            const int64_t need = n > 1 ? map_bytes(slabs, n) + B * D * (int64_t)sizeof(float) : 0;
             most = need > most ? need : most;
         }
     return most;
@@ -1181,6 +1186,14 @@ cudaError_t walk(Args &a, int dtype, void *work, cudaStream_t st)
     a.segments = (uint32_t)segments;
     a.per = (uint32_t)up(chunks, segments);
     a.maps = (Map2 *)work;
+    if (segments > 1 && a.first && a.first == a.last) {
+        // every segment begins from it, and the last may end before another begins
+        float *kept = (float *)((char *)work + map_bytes(slabs, segments));
+        const cudaError_t e = cudaMemcpyAsync(kept, a.first, (size_t)(a.B * a.D) * sizeof(float), cudaMemcpyDeviceToDevice, st);
+        if (e != cudaSuccess)
+            return e;
+        a.first = kept;
+    }
     const int64_t n = a.flat ? a.B * a.D : a.D, sequences = a.flat ? 1 : a.B;
     // rows of whole 16-byte pieces, a whole chunk of them at least
     bool tma = n * (int64_t)sizeof(T) % 16 == 0 && a.T >= kRun * kRuns && n < (int64_t(1) << 31) &&

@@ -1,6 +1,8 @@
-"""The policy operators at their edges: NaN among the alternatives of long rows."""
+"""The policy operators at their edges: NaN among the alternatives of long rows, a state that is written where it was
+read."""
 from __future__ import annotations
 
+import ctypes
 import math
 
 import pytest
@@ -8,6 +10,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests import test_gpu_policy_logp as logp  # noqa: E402
+from tests import test_gpu_policy_scan as scan  # noqa: E402
 from tests.policy_ref import BF16, F32, top_of  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -38,3 +41,34 @@ def test_nan_at_the_first_entry_of_a_long_row(pol, V, rows, dtype):
         there = torch.ones(5, V, dtype=torch.bool) if m is None else m[:5].cpu() != 0
         got = pol.log_probs(x, tok, mask=m, top=7)["top_index"][:5].cpu()
         assert torch.equal(got, top_of(x[:5].cpu().double(), there, 7))
+
+
+@pytest.mark.parametrize("T,B,D,dtype", [(512, 1, 256, BF16), (5000, 1, 64, F32), (700, 3, 65, BF16), (20, 3, 64, F32),
+                                         (6, 64, 64, BF16), (1, 3, 64, F32)])
+def test_state_in_its_place(pol, T, B, D, dtype):
+    """h_last may be h0 itself, and dh0 dlast: what C callers that step on do.  Long sequences are cut into segments, all
+    of which begin from that state; other work on the GPU makes some of them begin late."""
+    import paper_2407_04221_gb300 as av
+    L = av.load()
+    g, v, reset, h0, dh, dlast = scan.make(T, B, D, dtype, 0.001, T, shift=4.0)
+    want_h, want_last, states = pol.scan(g, v, reset, h0, save=True)
+    want = pol.scan_grad(dh, g, v, reset, states, dlast=dlast)
+    kind = {F32: 0, BF16: 1}[dtype]
+    n_states, n_work = ctypes.c_int64(), ctypes.c_int64()
+    assert L.av_scan_sizes(T, B, D, kind, ctypes.byref(n_states), ctypes.byref(n_work)) == 0
+    work = torch.empty(max(n_work.value, 16), dtype=torch.uint8, device="cuda")
+    h, dg, dv, kept = torch.empty_like(g), torch.empty_like(g), torch.empty_like(g), torch.empty_like(states)
+    busy, side = torch.randn(4096, 4096, device="cuda"), torch.cuda.Stream()
+    st, t, b = torch.cuda.current_stream().cuda_stream, B * D, D
+    for k in range(20):
+        state, flow = h0.clone(), dlast.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            busy @ busy
+        args = [g.data_ptr(), t, b, v.data_ptr(), t, b, reset.data_ptr(), B, 1]
+        assert L.av_scan(T, B, D, kind, *args, state.data_ptr(), h.data_ptr(), t, b, state.data_ptr(), kept.data_ptr(),
+                         work.data_ptr(), n_work.value, st) == 0
+        assert L.av_scan_grad(T, B, D, kind, dh.data_ptr(), t, b, *args, kept.data_ptr(), flow.data_ptr(), dg.data_ptr(),
+                              t, b, dv.data_ptr(), t, b, flow.data_ptr(), work.data_ptr(), n_work.value, st) == 0
+        for got, right in zip((h, state, kept, dg, dv, flow), (want_h, want_last, states, *want)):
+            assert torch.equal(got, right), (k, T)
