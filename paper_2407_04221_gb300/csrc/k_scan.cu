@@ -1140,7 +1140,7 @@ int64_t slabs_of(int64_t B, int64_t D, bool flat) { return flat ? up(B * D, kSla
 // (16.7 and 19.2); of two, 4 slabs 8.5 and 8.6.
 int64_t segments_of(int64_t slabs, int64_t chunks, int64_t resident)
 {
-    if (3 * slabs > resident || chunks <= 3 || (chunks <= 6 && 8 * slabs > resident))
+    if (slabs == 0 || 3 * slabs > resident || chunks <= 3 || (chunks <= 6 && 8 * slabs > resident))
         return 1;
     const int64_t most = resident / slabs, per = up(chunks, most < chunks ? most : chunks);
     return up(chunks, per);

@@ -72,3 +72,13 @@ def test_state_in_its_place(pol, T, B, D, dtype):
                               t, b, dv.data_ptr(), t, b, flow.data_ptr(), work.data_ptr(), n_work.value, st) == 0
         for got, right in zip((h, state, kept, dg, dv, flow), (want_h, want_last, states, *want)):
             assert torch.equal(got, right), (k, T)
+
+
+@pytest.mark.parametrize("T", [4, 1000, 20000])
+@pytest.mark.parametrize("B,D", [(0, 256), (4, 0)])
+def test_scan_of_an_empty_batch(pol, T, B, D):
+    g, v, reset, h0, dh, dlast = scan.make(T, B, D, BF16, 0.1, T)
+    h, last, states = pol.scan(g, v, reset, h0, save=True)
+    assert h.shape == (T, B, D) and last.shape == (B, D) and states.numel() == 0
+    dg, dv, dh0 = pol.scan_grad(dh, g, v, reset, states, dlast=dlast)
+    assert dg.shape == dv.shape == (T, B, D) and dh0.shape == (B, D)
