@@ -28,6 +28,7 @@ constexpr int kSms = 152;
 constexpr int kLongest = 16384;      // values of a row kept in registers
 constexpr int kLongThreads = 512;    // for longer rows
 constexpr int kColumns = 32;         // columns of a block that adds column sums
+constexpr int kMostShared = 227 * 1024 - 2048;  // bytes a block asks for at most: what it can have beside its fixed arrays
 
 // An array of parameters of either type, absent: `otherwise`.
 __device__ __forceinline__ float param(const void *p, int type, int i, float otherwise)
@@ -949,7 +950,7 @@ Room room_of(const Shape &s, int n, int e, bool back)
     const int sums = back ? 2 * s.per * s.group * 4 : 0;  // (over the rows' tiles)
     Room m{};
     for (m.resident = s.resident; m.resident > 0; --m.resident) {
-        m.deep = ((227 * 1024) / m.resident - 2048 - fixed) / row;
+        m.deep = ((kMostShared + 2048) / m.resident - 2048 - fixed) / row;
         if (m.deep >= (m.resident > 1 ? 3 : 1))
             break;
     }
@@ -986,6 +987,14 @@ int parts_of(int64_t rows, int n, int e, bool wide)
 bool packs(int64_t rows, int n, int e, const void *p, int64_t stride)
 {
     return n % (16 / e) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (rows <= 1 || stride * e % 16 == 0);
+}
+
+// Lets a kernel have what any of its launches asks for: the limit is the
+// kernel's and not the call's, so that calls from several threads all set the same.
+template <class K>
+cudaError_t let_share(K kernel)
+{
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
 }
 
 // Calls f with a shape's values a thread, threads a group (0: whole warps),
@@ -1065,7 +1074,7 @@ cudaError_t launch_norm(int64_t rows, int n, int dtype, int param_dtype, float e
             const Shape s = ring_of(n, eights, false);
             const Room room = room_of(s, n, sizeof(T), false);
             auto run = [&](auto kernel) {
-                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room.bytes);
+                e = let_share(kernel);
                 if (e == cudaSuccess)
                     kernel<<<blocks, s.block, room.bytes, st>>>(rows, n, s.group, eps, (const T *)x, x_stride, weight,
                                                                 bias, param_dtype, (T *)y, y_stride, mean, rstd,
@@ -1091,7 +1100,7 @@ cudaError_t launch_norm(int64_t rows, int n, int dtype, int param_dtype, float e
         const int shared = 2 * s.per * s.group * 4;
         auto run = [&](auto kernel) {
             if (shared > 40 * 1024)
-                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+                e = let_share(kernel);
             if (e == cudaSuccess)
                 kernel<<<blocks, s.block, shared, st>>>(rows, n, s.group, eps, (const T *)x, x_stride, weight, bias,
                                                         param_dtype, (T *)y, y_stride, mean, rstd);
@@ -1142,7 +1151,7 @@ cudaError_t launch_norm_grad(int64_t rows, int n, int dtype, int param_dtype, co
                 const Shape s = ring_of(n, eights, true);
                 const Room room = room_of(s, n, sizeof(T), true);
                 auto run = [&](auto kernel) {
-                    bad = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, room.bytes);
+                    bad = let_share(kernel);
                     if (bad == cudaSuccess)
                         kernel<<<blocks, s.block, room.bytes, st>>>(rows, n, s.group, (const T *)dy, dy_stride,
                                                                     (const T *)x, x_stride, weight, param_dtype, mean,
@@ -1167,7 +1176,7 @@ cudaError_t launch_norm_grad(int64_t rows, int n, int dtype, int param_dtype, co
             const int shared = (s.per * s.group + sums_at) * 4;
             auto run = [&](auto kernel) {
                 if (shared > 40 * 1024)
-                    bad = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+                    bad = let_share(kernel);
                 if (bad == cudaSuccess)
                     kernel<<<blocks, s.block, shared, st>>>(rows, n, s.group, (const T *)dy, dy_stride, (const T *)x,
                                                             x_stride, weight, param_dtype, mean, rstd, (T *)dx,

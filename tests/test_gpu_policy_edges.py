@@ -1,15 +1,17 @@
 """The policy operators at their edges: NaN among the alternatives of long rows, a state that is written where it was
-read."""
+read, calls from two threads."""
 from __future__ import annotations
 
 import ctypes
 import math
+import threading
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
 from tests import test_gpu_policy_logp as logp  # noqa: E402
+from tests import test_gpu_policy_norm as norm  # noqa: E402
 from tests import test_gpu_policy_scan as scan  # noqa: E402
 from tests.policy_ref import BF16, F32, top_of  # noqa: E402
 
@@ -82,3 +84,27 @@ def test_scan_of_an_empty_batch(pol, T, B, D):
     assert h.shape == (T, B, D) and last.shape == (B, D) and states.numel() == 0
     dg, dv, dh0 = pol.scan_grad(dh, g, v, reset, states, dlast=dlast)
     assert dg.shape == dv.shape == (T, B, D) and dh0.shape == (B, D)
+
+
+@pytest.mark.parametrize("gradient", [False, True])
+def test_rows_of_two_lengths_from_two_threads(pol, gradient):
+    """Two threads with rows that take one kernel and different amounts of shared memory."""
+    wrong = []
+
+    def work(n):
+        try:
+            x, dy, w, b = norm.make(64, n, BF16, F32, n)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                _, mean, rstd = pol.layer_norm(x, w, b)
+                for _ in range(3000):
+                    pol.layer_norm_grad(dy, x, w, mean, rstd) if gradient else pol.layer_norm(x, w, b)
+        except Exception as e:  # noqa: BLE001
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in (1024, 4096)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong
