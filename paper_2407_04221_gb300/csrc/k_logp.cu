@@ -722,7 +722,7 @@ __global__ __launch_bounds__(kGradThreads) void logp_wide_grad_kernel(const Logp
     T *dx = dlogits + r * dstride;
     const int thread = threadIdx.x % kLanes + blockIdx.y * kLanes, step = kLanes * gridDim.y;
     if (!packed) {  // dlogits' rows begin elsewhere in 16 bytes than those of logits
-        for (int j = thread; j < a.V; j += step)
+        for (uint32_t j = thread; j < (uint32_t)a.V; j += step)  // (the last step may go beyond an int)
             dx[j] = from_f32<T>(gradient_at<kMask>(s, row.template entry<kMask>(j), j));
         return;
     }

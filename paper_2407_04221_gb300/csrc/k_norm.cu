@@ -767,7 +767,8 @@ __device__ float long_sum(float v, float *s)
     return t;
 }
 
-// A block a row, read three times, twice from L2: 1,500 rows of 20,011 16-bit
+// A block a row, read three times, twice from L2 (counted down: the last step
+// up of a row of 2^31 - 1 values would go beyond an int): 1,500 rows of 20,011 16-bit
 // values 72 us, the gradient with the columns' sums 205.
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(int64_t rows, int n, float eps, const T *x, int64_t xs,
@@ -779,19 +780,22 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(int64_t rows, i
         const T *xr = x + r * xs;
         float v = 0.0f;
 #pragma unroll 8
-        for (int i = threadIdx.x; i < n; i += kLongThreads)
-            v += to_f32(xr[i]);
+        for (int left = n - (int)threadIdx.x; left > 0; left -= kLongThreads)
+            v += to_f32(xr[n - left]);
         const float m = long_sum(v, s) / n;
         v = 0.0f;
 #pragma unroll 8
-        for (int i = threadIdx.x; i < n; i += kLongThreads) {
+        for (int left = n - (int)threadIdx.x; left > 0; left -= kLongThreads) {
+            const int i = n - left;
             const float c = to_f32(xr[i]) - m;
             v += c * c;
         }
         const float q = 1.0f / sqrtf(long_sum(v, s) / n + eps);
 #pragma unroll 8
-        for (int i = threadIdx.x; i < n; i += kLongThreads)
+        for (int left = n - (int)threadIdx.x; left > 0; left -= kLongThreads) {
+            const int i = n - left;
             y[r * ys + i] = from_f32<T>((to_f32(xr[i]) - m) * q * param(w, ptype, i, 1.0f) + param(b, ptype, i, 0.0f));
+        }
         if (mean && threadIdx.x == 0) {
             mean[r] = m;
             rstd[r] = q;
@@ -811,7 +815,8 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_dx_kernel(int64_t rows
         const float m = mean[r], q = rstd[r];
         float a = 0.0f, c = 0.0f;
 #pragma unroll 8
-        for (int i = threadIdx.x; i < n; i += kLongThreads) {
+        for (int left = n - (int)threadIdx.x; left > 0; left -= kLongThreads) {
+            const int i = n - left;
             const float d = to_f32(dr[i]) * param(w, ptype, i, 1.0f);
             a += d;
             c += d * (to_f32(xr[i]) - m) * q;
@@ -819,7 +824,8 @@ __global__ __launch_bounds__(kLongThreads) void norm_long_dx_kernel(int64_t rows
         a = long_sum(a, s) / n;
         c = long_sum(c, s) / n;
 #pragma unroll 8
-        for (int i = threadIdx.x; i < n; i += kLongThreads) {
+        for (int left = n - (int)threadIdx.x; left > 0; left -= kLongThreads) {
+            const int i = n - left;
             const float d = to_f32(dr[i]) * param(w, ptype, i, 1.0f);
             dx[r * dxs + i] = from_f32<T>(q * (d - a - (to_f32(xr[i]) - m) * q * c));
         }
@@ -974,7 +980,7 @@ int blocks_of(int64_t rows, int n, int e, bool wide, bool back)
 // Rows' parts of the column sums of long rows: blocks for every SM, eight rows each at least.
 int long_parts(int64_t rows, int n)
 {
-    const int64_t slabs = (n + 31) / 32, want = (8 * kSms + slabs - 1) / slabs, most = (rows + 7) / 8;
+    const int64_t slabs = ((int64_t)n + 31) / 32, want = (8 * kSms + slabs - 1) / slabs, most = (rows + 7) / 8;
     return (int)(want < most ? want : most);
 }
 
@@ -1142,7 +1148,7 @@ cudaError_t launch_norm_grad(int64_t rows, int n, int dtype, int param_dtype, co
                                                                         (const T *)x, x_stride, weight, param_dtype,
                                                                         mean, rstd, (T *)dx, dx_stride);
                 if (sums)
-                    norm_long_columns_kernel<T><<<dim3((n + 31) / 32, count), 256, 0, st>>>(
+                    norm_long_columns_kernel<T><<<dim3((unsigned)(((int64_t)n + 31) / 32), count), 256, 0, st>>>(
                         rows, n, (const T *)dy, dy_stride, (const T *)x, x_stride, mean, rstd, parts);
                 return cudaGetLastError();
             }
@@ -1199,7 +1205,7 @@ cudaError_t launch_norm_grad(int64_t rows, int n, int dtype, int param_dtype, co
             return e;
     }
     if (sums)
-        return launch_chained(norm_columns_kernel, dim3((n + kColumns - 1) / kColumns, 2), 256, 0, st, rows > 0, count, n,
+        return launch_chained(norm_columns_kernel, dim3((unsigned)(((int64_t)n + kColumns - 1) / kColumns), 2), 256, 0, st, rows > 0, count, n,
                               parts, param_dtype, dweight, dbias);
     return cudaSuccess;
 }

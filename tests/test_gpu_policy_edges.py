@@ -1,5 +1,5 @@
 """The policy operators at their edges: NaN among the alternatives of long rows, a state that is written where it was
-read, calls from two threads."""
+read, calls from two threads, rows of 2^31 - 1 values."""
 from __future__ import annotations
 
 import ctypes
@@ -108,3 +108,47 @@ def test_rows_of_two_lengths_from_two_threads(pol, gradient):
         t.join()
     torch.cuda.synchronize()
     assert not wrong
+
+
+LONGEST = 2**31 - 1
+
+
+def room():
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 80 * 2**30:
+        pytest.skip("not enough memory")
+
+
+def test_norm_of_the_longest_row(pol):
+    """Ones of alternating signs, one more of +1: mean 2^-31, variance 1, so y is x and xh is x to 2^-17 (eps)."""
+    room()
+    x = torch.ones(1, LONGEST, dtype=BF16, device="cuda")
+    x[0, 1::2] = -1
+    y, mean, rstd = pol.layer_norm(x)
+    assert torch.equal(y, x) and abs(float(mean)) < 1e-6 and abs(float(rstd) - 1) < 1e-5
+    del y
+    dx, dw, db = pol.layer_norm_grad(x, x, None, mean, rstd)
+    assert float(dx.abs().max()) < 1e-4  # (what is left of d - xh mean(d xh))
+    assert float((dw - 1).abs_().max()) < 1e-4
+    assert float(db[0]) == float(db[-1]) == 1 and float(db[1]) == -1 and float(db.abs_().min()) == 1
+    del x, dx, dw, db
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("start", [0, 1])
+def test_log_probs_of_the_longest_row(pol, start):
+    """Zeros and a last entry of 20, its token: sums of 2^21 equal terms a thread are exact to 2^-24."""
+    room()
+    x = torch.zeros(LONGEST + start, dtype=BF16, device="cuda")[None, start:]
+    x[0, -1] = 20
+    tok = torch.tensor([LONGEST - 1], device="cuda")
+    out = pol.log_probs(x, tok, top=2)
+    rest = (LONGEST - 1) * math.exp(-20)
+    assert out["top_index"].tolist() == [[LONGEST - 1, 0]] and float(out["peak"]) == 20
+    assert abs(float(out["logz"]) - math.log1p(rest)) < 1e-4 and abs(float(out["logp"]) + math.log1p(rest)) < 1e-4
+    dx = pol.log_probs_grad(torch.ones(1, device="cuda"), None, x, tok, out)
+    p = math.exp(-20) / (1 + rest)
+    assert abs(float(dx[0, -1]) / (rest / (1 + rest)) - 1) < 2**-8 + 1e-4
+    assert abs(float(dx[0, :-1].min()) / -p - 1) < 2**-8 + 1e-4 and abs(float(dx[0, :-1].max()) / -p - 1) < 2**-8 + 1e-4
+    del x, dx
+    torch.cuda.empty_cache()
