@@ -15,7 +15,10 @@ __device__ __forceinline__ uint64_t now_ns()
     return t;
 }
 
-constexpr uint64_t kGiveUpNs = 4000000000ull;
+#ifndef AV_GIVE_UP_NS
+#define AV_GIVE_UP_NS 4000000000ull
+#endif
+constexpr uint64_t kGiveUpNs = AV_GIVE_UP_NS;
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count)
 {

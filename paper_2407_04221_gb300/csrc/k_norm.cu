@@ -565,8 +565,10 @@ __global__ __launch_bounds__(kMost, kMin) void norm_ring_kernel(int64_t rows, in
             t = add2(t, v[k]);
         }
         float sum[1] = {t.x + t.y};
+        if (!ok)  // (past a wait that ran out: no wrong row passes for a right one)
+            sum[0] = __int_as_float(0x7fffffff);
         group_sum<0>(sum, g, slots, turn);
-        if (g.thread == 0)  // (all of the group have read the row)
+        if (g.thread == 0 && ok)  // (all of the group have read the row)
             ring.fetch(r + deep * ring.step, stage);
         if (++stage == deep) {
             stage = 0;
@@ -595,9 +597,7 @@ __global__ __launch_bounds__(kMost, kMin) void norm_ring_kernel(int64_t rows, in
             }
         }
         group_sum<0>(square, g, slots, turn);
-        float q = 1.0f / sqrtf(square[0] * per + eps);
-        if (!ok)  // (past a wait that ran out: no wrong row passes for a right one)
-            q = __int_as_float(0x7fffffff);
+        const float q = 1.0f / sqrtf(square[0] * per + eps);
         T *out = y + r * ys;
 #pragma unroll
         for (int c = 0; c < kPacks; c += kVec == 1 ? 2 : 1) {
@@ -698,15 +698,15 @@ __global__ __launch_bounds__(kMost, kMin) void norm_grad_ring_kernel(int64_t row
             s1 = fma2(d, xh, s1);
         }
         float s[2] = {s0.x + s0.y, s1.x + s1.y};
+        if (!ok)
+            s[0] = __int_as_float(0x7fffffff);
         group_sum<0>(s, g, slots, turn);
-        if (g.thread == 0)
+        if (g.thread == 0 && ok)
             ring.fetch(r + deep * ring.step, stage);
         if (++stage == deep) {
             stage = 0;
             phase ^= 1;
         }
-        if (!ok)
-            s[0] = __int_as_float(0x7fffffff);
         const float2 a = make_float2(-s[0] * per * q, -s[0] * per * q), c1 = make_float2(-s[1] * per * q, -s[1] * per * q);
         T *out = dx + r * dxs;
 #pragma unroll
@@ -725,7 +725,9 @@ __global__ __launch_bounds__(kMost, kMin) void norm_grad_ring_kernel(int64_t row
     }
     if (!ok) {
         linger();
-        dw[0].x = db[0].x = __int_as_float(0x7fffffff);
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k)
+            dw[k] = db[k] = make_float2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
     }
     if (!parts)
         return;

@@ -1,0 +1,94 @@
+"""A wait for a copy that does not end (tests/late_copies.cu): the call returns, and whatever the missing bytes would have
+touched is NaN, so that nothing wrong passes for right."""
+from __future__ import annotations
+
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests import test_gpu_policy_norm as norm  # noqa: E402
+from tests.policy_ref import BF16, F32  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def late(tmp_path_factory):
+    """late(source): the library with that operator's kernels compiled so, argument types as the package's."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2407_04221_gb300 as av
+    from paper_2407_04221_gb300 import build, policy
+    policy._load()
+    ours, at = av.load(), tmp_path_factory.mktemp("late")
+
+    def made(source):
+        lib = at / (source + ".so")
+        subprocess.check_call([build.nvcc(), "-shared", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", *build.ARCH, "-cudart",
+                               "shared", "-I", os.path.join(build.ROOT, "include"), "-I", build.CSRC,
+                               f'-DAV_SOURCE="{source}"', os.path.join(HERE, "late_copies.cu"), "-o", str(lib),
+                               "-L", build.PKG, "-l:libautoverse.so", "-Xlinker", "-rpath", "-Xlinker", build.PKG])
+        L = ctypes.CDLL(str(lib))
+        for name in av.EXPORTS:
+            if hasattr(L, name):
+                getattr(L, name).argtypes = getattr(ours, name).argtypes
+        return L
+
+    return made
+
+
+@pytest.fixture(scope="module")
+def pol(late):
+    from paper_2407_04221_gb300 import policy
+    return policy
+
+
+@pytest.fixture(scope="module")
+def late_norm(late):
+    return late("k_norm.cu")
+
+
+def right_or_nan(got, right):
+    """Of rows of values: which are right throughout; the others are NaN throughout."""
+    good, bad = (got == right).all(-1), torch.isnan(got).all(-1)
+    assert (good | bad).all()
+    return good
+
+
+@pytest.mark.parametrize("n,dtype", [(1024, BF16), (1001, F32), (4805, F32)])
+def test_layer_norm(pol, late_norm, n, dtype):
+    rows = 6000
+    x, dy, w, b = norm.make(rows, n, dtype, F32, n)
+    kind, st = {F32: 0, BF16: 1}[dtype], torch.cuda.current_stream().cuda_stream
+    right = pol.layer_norm(x, w, b)
+    grads = pol.layer_norm_grad(dy, x, w, *right[1:])
+    y, mean, rstd = (torch.zeros_like(t) for t in right)
+    for nth in (0, 1):  # (a group takes two rows at least)
+        assert late_norm.set_late(1, nth) == 0
+        assert late_norm.av_layer_norm(rows, n, kind, 0, norm.EPS, x.data_ptr(), n, w.data_ptr(), b.data_ptr(),
+                                       y.data_ptr(), n, mean.data_ptr(), rstd.data_ptr(), st) == 0
+        torch.cuda.synchronize()
+        good = right_or_nan(y, right[0])
+        assert 0 < int((~good).sum()) < rows // 2
+        for got, want in ((mean, right[1]), (rstd, right[2])):
+            assert torch.equal(got[good], want[good]) and torch.isnan(got[~good]).all()
+        dx, dw, db = (torch.zeros_like(t) for t in grads)
+        need = ctypes.c_int64()
+        assert late_norm.av_layer_norm_work(rows, n, ctypes.byref(need)) == 0
+        work = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+        assert late_norm.set_late(1, nth) == 0
+        assert late_norm.av_layer_norm_grad(rows, n, kind, 0, dy.data_ptr(), n, x.data_ptr(), n, w.data_ptr(),
+                                            right[1].data_ptr(), right[2].data_ptr(), dx.data_ptr(), n, dw.data_ptr(),
+                                            db.data_ptr(), work.data_ptr(), need.value, st) == 0
+        torch.cuda.synchronize()
+        assert 0 < int((~right_or_nan(dx, grads[0])).sum()) < rows // 2
+        assert torch.isnan(dw).all() and torch.isnan(db).all()
+    assert late_norm.set_late(-1, 0) == 0  # (no block's)
+    assert late_norm.av_layer_norm(rows, n, kind, 0, norm.EPS, x.data_ptr(), n, w.data_ptr(), b.data_ptr(), y.data_ptr(), n,
+                                   mean.data_ptr(), rstd.data_ptr(), st) == 0
+    assert torch.equal(y, right[0])
