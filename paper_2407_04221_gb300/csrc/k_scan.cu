@@ -813,9 +813,15 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
         if (kTma)
             asm volatile("cp.async.wait_group 0;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (before copies to where this thread read or wrote)
-        __syncthreads();  // this chunk is here, the one before is done with
+        ok = __syncthreads_and(ok);  // this chunk is here, the one before is done with
         const int s_next = s + 1 == kStages ? 0 : s + 1;
-        fill(items[(i + 1) & 3], s_next);
+        if (ok) {
+            fill(items[(i + 1) & 3], s_next);
+        } else if (kTma && kOut > 0) {  // (what left from this stage has been read)
+            if (threadIdx.x == 0)
+                asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncthreads();
+        }
         if (threadIdx.x == 0)
             order.next(a, items[(i + 2) & 3]);
         const Item item = items[i & 3];
@@ -843,7 +849,8 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
             }
         }();
         Run<kBack, kRun> run;
-        run.resets = resets_of<kRun>(a, item, c.t0, c.steps);
+        // (past a wait that ran out nothing is known of the steps, and no begin of an episode ends the NaN)
+        run.resets = ok ? resets_of<kRun>(a, item, c.t0, c.steps) : 0;
         run.plain = __all_sync(~0u, run.resets == 0);
         if constexpr (kMapsOnly) {
             const Map2 m = kBack ? whole<true>(joined<true>(run.flow_map(tile))) : whole<false>(joined<false>(run.gates(tile)));
@@ -880,6 +887,8 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void w
             if (kBack) {
                 const float *kept = c.kept(a, item, channel);
                 h = make_float2(c.first ? kept[0] : 0.0f, c.second ? kept[1] : 0.0f);
+                if (!ok)
+                    h = make_float2(carry[0], carry[1]);
             } else {
                 h = make_float2(carry[0], carry[1]);
                 if (a.states && speaks) {

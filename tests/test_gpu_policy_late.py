@@ -11,6 +11,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests import test_gpu_policy_norm as norm  # noqa: E402
+from tests import test_gpu_policy_scan as scan  # noqa: E402
 from tests.policy_ref import BF16, F32  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -92,3 +93,49 @@ def test_layer_norm(pol, late_norm, n, dtype):
     assert late_norm.av_layer_norm(rows, n, kind, 0, norm.EPS, x.data_ptr(), n, w.data_ptr(), b.data_ptr(), y.data_ptr(), n,
                                    mean.data_ptr(), rstd.data_ptr(), st) == 0
     assert torch.equal(y, right[0])
+
+
+def some_nan(got, right, least=1, most=0.5):
+    """Values are right or NaN; how many are NaN is within least and a share of them."""
+    bad = got != right
+    assert torch.isnan(got[bad]).all() and least <= int(bad.sum()) <= most * bad.numel()
+
+
+@pytest.fixture(scope="module")
+def late_scan(late):
+    return late("k_scan.cu")
+
+
+@pytest.mark.parametrize("T,B,D,dtype", [(700, 400, 64, BF16), (700, 400, 65, BF16), (700, 400, 66, BF16),
+                                         (700, 400, 64, F32), (3001, 8, 64, BF16), (3001, 8, 65, F32)])
+@pytest.mark.parametrize("resets", [0.0, 0.02])
+def test_scan(pol, late_scan, T, B, D, dtype, resets):
+    """By tensor copies and by rows, whole and in segments (the last two).  Begins of episodes do not end the NaN within
+    a block, which knows nothing of the steps that it missed."""
+    g, v, reset, h0, dh, dlast = scan.make(T, B, D, dtype, resets, T + D, shift=3.0)
+    kind, st = {F32: 0, BF16: 1}[dtype], torch.cuda.current_stream().cuda_stream
+    h, last, states = pol.scan(g, v, reset, h0, save=True)
+    grads = pol.scan_grad(dh, g, v, reset, states, dlast=dlast)
+    sizes = ctypes.c_int64(), ctypes.c_int64()
+    assert late_scan.av_scan_sizes(T, B, D, kind, *(ctypes.byref(n) for n in sizes)) == 0
+    work = torch.empty(max(16, sizes[1].value), dtype=torch.uint8, device="cuda")
+    t, b = B * D, D
+    args = [g.data_ptr(), t, b, v.data_ptr(), t, b, reset.data_ptr(), B, 1]
+    for nth in (0, 1):
+        got = [torch.zeros_like(x) for x in (h, last, states)]
+        assert late_scan.set_late(1, nth) == 0
+        assert late_scan.av_scan(T, B, D, kind, *args, h0.data_ptr(), got[0].data_ptr(), t, b, got[1].data_ptr(),
+                                 got[2].data_ptr(), work.data_ptr(), sizes[1].value, st) == 0
+        torch.cuda.synchronize()
+        some_nan(got[0], h)
+        some_nan(got[1], last, 0)
+        some_nan(got[2], states, 0)
+        got = [torch.zeros_like(x) for x in grads]
+        assert late_scan.set_late(1, nth) == 0
+        assert late_scan.av_scan_grad(T, B, D, kind, dh.data_ptr(), t, b, *args, states.data_ptr(), dlast.data_ptr(),
+                                      got[0].data_ptr(), t, b, got[1].data_ptr(), t, b, got[2].data_ptr(), work.data_ptr(),
+                                      sizes[1].value, st) == 0
+        torch.cuda.synchronize()
+        some_nan(got[0], grads[0])
+        some_nan(got[1], grads[1])
+        some_nan(got[2], grads[2], 0)
