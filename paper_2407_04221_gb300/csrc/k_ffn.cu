@@ -545,11 +545,13 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
         const uint32_t slab0 = slabs + team * kSlabs * kSlab;
         const float scale = kScaled<T> && kForm != kForward ? scale_of(p.peaks) : 1.0f, back = 1.0f / scale;
         int done = 0;
+        bool ok = true;
         for (int i = pair; i < tiles; i += pairs, ++done) {
             const Tile t = tile_of(p, i);
             const int set = done & 1;
-            // (past a wait that ran out the outputs are NaN, so that no wrong result passes for a right one)
-            const bool ok = __all_sync(~0u, bar_wait(acc_full + 8 * set, done >> 1 & 1, dead));
+            // (past a wait that ran out the outputs are NaN, so that no wrong result passes for a right one: also those
+            // of later tiles, whose products never start, though the barrier shows the parity they wait for)
+            ok = __all_sync(~0u, ok && bar_wait(acc_full + 8 * set, done >> 1 & 1, dead));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + set * kTile + ((uint32_t)(quarter * 32) << 16);
             const int m0 = t.m * kTile + rank * kRowsCta;

@@ -5,14 +5,16 @@ from __future__ import annotations
 import ctypes
 import os
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
 torch = pytest.importorskip("torch")
 
+from tests import test_gpu_policy_ffn as ffn  # noqa: E402
 from tests import test_gpu_policy_norm as norm  # noqa: E402
 from tests import test_gpu_policy_scan as scan  # noqa: E402
-from tests.policy_ref import BF16, F32  # noqa: E402
+from tests.policy_ref import BF16, F16, F32  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -20,7 +22,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 
 @pytest.fixture(scope="module")
 def late(tmp_path_factory):
-    """late(source): the library with that operator's kernels compiled so, argument types as the package's."""
+    """The libraries with an operator's kernels compiled so, argument types as the package's, by their source."""
     if not torch.cuda.is_available():
         pytest.skip("no CUDA device")
     import paper_2407_04221_gb300 as av
@@ -40,7 +42,9 @@ def late(tmp_path_factory):
                 getattr(L, name).argtypes = getattr(ours, name).argtypes
         return L
 
-    return made
+    sources = ("k_norm.cu", "k_scan.cu", "k_ffn.cu")
+    with ThreadPoolExecutor(len(sources)) as pool:
+        return dict(zip(sources, pool.map(made, sources)))
 
 
 @pytest.fixture(scope="module")
@@ -51,7 +55,7 @@ def pol(late):
 
 @pytest.fixture(scope="module")
 def late_norm(late):
-    return late("k_norm.cu")
+    return late["k_norm.cu"]
 
 
 def right_or_nan(got, right):
@@ -103,7 +107,7 @@ def some_nan(got, right, least=1, most=0.5):
 
 @pytest.fixture(scope="module")
 def late_scan(late):
-    return late("k_scan.cu")
+    return late["k_scan.cu"]
 
 
 @pytest.mark.parametrize("T,B,D,dtype", [(700, 400, 64, BF16), (700, 400, 65, BF16), (700, 400, 66, BF16),
@@ -139,3 +143,37 @@ def test_scan(pol, late_scan, T, B, D, dtype, resets):
         some_nan(got[0], grads[0])
         some_nan(got[1], grads[1])
         some_nan(got[2], grads[2], 0)
+
+
+@pytest.fixture(scope="module")
+def late_ffn(late):
+    return late["k_ffn.cu"]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,D,H", [(300, 136, 264), (9000, 264, 520), (40, 2056, 72)])
+def test_gated_ffn(pol, late_ffn, rows, D, H, dtype):
+    """One tile a pair of blocks, several, and terms in parts.  The first pair's copies come short, those of its first
+    CTA's first or a later stage: of h, of dg and du, of dx or of dw (by the count of stages before)."""
+    x, w, dh = ffn.make(rows, D, H, dtype, rows)
+    kind, st = {BF16: 1, F16: 2}[dtype], torch.cuda.current_stream().cuda_stream
+    right, grads = pol.gated_ffn(x, w), pol.gated_ffn_grad(dh, x, w)
+    need = ctypes.c_int64()
+    assert late_ffn.av_gated_ffn_work(rows, D, H, ctypes.byref(need)) == 0
+    work = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+    blocks = -(-D // 64)
+    for nth in (0, blocks - 1, blocks + 1):
+        h = torch.zeros_like(right)
+        assert late_ffn.set_late(0, nth) == 0
+        assert late_ffn.av_gated_ffn(rows, D, H, kind, 0, x.data_ptr(), D, w.data_ptr(), h.data_ptr(), H, st) == 0
+        torch.cuda.synchronize()
+        some_nan(h, right, 0 if nth > blocks else 1, 1.0)
+    for nth in (0, blocks, blocks + 2, blocks + 40, blocks + 90):
+        dx, dw = (torch.zeros_like(t) for t in grads)
+        assert late_ffn.set_late(0, nth) == 0
+        assert late_ffn.av_gated_ffn_grad(rows, D, H, kind, 0, dh.data_ptr(), H, x.data_ptr(), D, w.data_ptr(),
+                                          dx.data_ptr(), D, dw.data_ptr(), work.data_ptr(), need.value, st) == 0
+        torch.cuda.synchronize()
+        some_nan(dx, grads[0], 0, 1.0)
+        some_nan(dw, grads[1], 0, 1.0)
+        assert nth > 0 or (torch.isnan(dx).any() and torch.isnan(dw).any())
