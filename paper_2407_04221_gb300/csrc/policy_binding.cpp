@@ -7,6 +7,7 @@
 // 17.3 us through ctypes and torch's Python functions and takes 5.9 here, some
 // four of them the library's call.
 // The functions take positional arguments only; policy.py is their face.
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <Python.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -537,6 +538,21 @@ PyObject *gated_ffn_grad(PyObject *const *a)
 
 // ------------------------------------------------------------ module
 
+// Results are detached.  Where autograd would have recorded the call, it says so;
+// false: the warning was made an error.
+bool warn_detached(PyObject *const *args, Py_ssize_t n)
+{
+    if (!c10::GradMode::is_enabled())
+        return true;
+    for (Py_ssize_t k = 0; k < n; ++k)
+        if (THPVariable_Check(args[k]) && THPVariable_Unpack(args[k]).requires_grad())
+            return PyErr_WarnEx(PyExc_UserWarning,
+                                "policy operators are not recorded by autograd: the results are detached from arguments "
+                                "that require gradients (call them under torch.no_grad() or in a torch.autograd.Function)",
+                                2) == 0;
+    return true;
+}
+
 // A function of exactly kArgs arguments; no exception leaves it.
 template <PyObject *(*fn)(PyObject *const *), Py_ssize_t kArgs>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -546,6 +562,8 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n)
         return nullptr;
     }
     HANDLE_TH_ERRORS
+    if (!warn_detached(args, n))
+        return nullptr;
     try {
         return fn(args);
     } catch (const Refused &e) {

@@ -9,6 +9,11 @@ library's `av_*` function of the same name (in `csrc/policy_binding.cpp`), whose
 Arrays are float32, bfloat16 or float16; innermost axes are contiguous, the
 others may have any strides, inputs also those of broadcast (expanded) arrays.
 
+Nothing is recorded by autograd: results are detached, and a call whose
+arguments require gradients warns of it where gradients are enabled.  Each
+gradient has a function of its own; `examples/recurrent_policy.py` makes
+`torch.autograd.Function`s of them.
+
 A function given a `stream` runs whole on it, as the calls of `Env` do: its
 outputs come from that stream's pool, its arguments are marked as used by that
 stream and its results as used by the current one.  It waits for nothing: the

@@ -1,10 +1,12 @@
 """The policy operators at their edges: NaN among the alternatives of long rows, a state that is written where it was
-read, calls from two threads, rows of 2^31 - 1 values."""
+read, calls from two threads, rows of 2^31 - 1 values, arguments
+that require gradients."""
 from __future__ import annotations
 
 import ctypes
 import math
 import threading
+import warnings
 
 import pytest
 
@@ -152,3 +154,41 @@ def test_log_probs_of_the_longest_row(pol, start):
     assert abs(float(dx[0, :-1].min()) / -p - 1) < 2**-8 + 1e-4 and abs(float(dx[0, :-1].max()) / -p - 1) < 2**-8 + 1e-4
     del x, dx
     torch.cuda.empty_cache()
+
+
+def test_detached_results_are_said(pol):
+    """Nothing is recorded by autograd: a call that it would have recorded warns, any other does not."""
+    x, dy, w, b = norm.make(8, 64, BF16, F32, 1)
+    tok = torch.zeros(8, dtype=torch.int64, device="cuda")
+    wants, ffn_w = x.clone().requires_grad_(), torch.zeros(2, 8, 64, dtype=BF16, device="cuda", requires_grad=True)
+    calls = [lambda: pol.layer_norm(x, torch.nn.Parameter(w), b), lambda: pol.layer_norm(wants), lambda: pol.log_probs(wants, tok),
+             lambda: pol.scan(x[None], wants[None]), lambda: pol.gated_ffn(x, ffn_w),
+             lambda: pol.layer_norm(wants, stream=torch.cuda.current_stream())]
+    for call in calls:
+        with pytest.warns(UserWarning, match="detached"):
+            got = call()
+        assert not any(t.requires_grad for t in (got.values() if isinstance(got, dict) else got))
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        with torch.no_grad():
+            for call in calls:
+                call()
+        pol.layer_norm(x, w, b)
+        pol.layer_norm(wants.detach())
+
+        class Norm(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x):
+                y, mean, rstd = pol.layer_norm(x)
+                ctx.save_for_backward(x, mean, rstd)
+                return y
+
+            @staticmethod
+            def backward(ctx, dy):
+                x, mean, rstd = ctx.saved_tensors
+                return pol.layer_norm_grad(dy, x, None, mean, rstd)[0]
+
+        Norm.apply(wants).backward(dy)
+        assert torch.isfinite(wants.grad).all()
+        with pytest.raises(UserWarning):
+            calls[1]()
