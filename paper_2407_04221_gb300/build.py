@@ -22,6 +22,7 @@ DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("kernels.cuh", "launch.h", "k_
     os.path.join(ROOT, "include", "autoverse.h")]
 BINDING = os.path.join(CSRC, "policy_binding.cpp")
 BINDING_LIB = os.path.join(PKG, "_policy.so")
+BINDING_STAMP = os.path.join(PKG, "_build", "policy_torch.txt")  # what it was made for
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -51,16 +52,34 @@ def _link_binding(obj: str, out: str) -> list:
             "-ltorch_cuda", "-ltorch_cpu", "-ltorch", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{libs}"]
 
 
+def _torch_stamp():
+    """Which torch the binding is made for; None without one."""
+    try:
+        import torch
+    except ImportError:
+        return None
+    return f"{torch.__version__} {os.path.abspath(torch.__file__)}\n"
+
+
+def _read(path):
+    try:
+        with open(path) as f:
+            return f.read()
+    except OSError:
+        return None
+
+
 def build(force: bool = False, verbose: bool = False, extra: list | None = None) -> str:
     """Build the shared library and the binding next to this file: every
-    translation unit is compiled in parallel, then linked.  Returns the
-    library's path."""
+    translation unit is compiled in parallel, then linked, the library first.
+    Without torch the library alone.  Returns the library's path."""
     def stale(lib, deps):
         return not os.path.exists(lib) or any(os.path.getmtime(d) > os.path.getmtime(lib) for d in deps)
 
     native = bool(force or extra) or stale(LIB, DEPS)
-    binding = native or stale(BINDING_LIB, [BINDING, LIB])
-    if not binding:
+    stamp = _torch_stamp()
+    binding = stamp is not None and (native or stale(BINDING_LIB, [BINDING, LIB]) or _read(BINDING_STAMP) != stamp)
+    if not (native or binding):
         return LIB
     import tempfile
     from concurrent.futures import ThreadPoolExecutor
@@ -73,21 +92,29 @@ def build(force: bool = False, verbose: bool = False, extra: list | None = None)
     cuda_lib = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "lib64")
     common = [nvcc(), "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-lineinfo", *ARCH,
               "-I", os.path.join(ROOT, "include"), *(extra or [])]
-    with tempfile.TemporaryDirectory() as tmpdir:
+    with tempfile.TemporaryDirectory() as tmpdir, ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
         sources = SOURCES if native else []
         objs = [os.path.join(tmpdir, os.path.basename(src) + ".o") for src in sources]
         glue = os.path.join(tmpdir, "policy_binding.o")
-        cmds = [common + ["-c", src, "-o", obj] for src, obj in zip(sources, objs)] + [_compile_binding(glue)]
-        with ThreadPoolExecutor(max_workers=len(cmds)) as pool:
-            list(pool.map(run, cmds))
+        units = [pool.submit(run, common + ["-c", src, "-o", obj]) for src, obj in zip(sources, objs)]
+        bound = pool.submit(lambda: run(_compile_binding(glue))) if binding else None
+        for unit in units:
+            unit.result()
         if native:
             tmp = LIB + f".tmp{os.getpid()}"
             run([nvcc(), "-shared", *ARCH, "-cudart", "shared", "-Xlinker", "-rpath", "-Xlinker", cuda_lib,
                  "-Xlinker", "-soname", "-Xlinker", os.path.basename(LIB), *objs, "-o", tmp])
             os.replace(tmp, LIB)
-        tmp = BINDING_LIB + f".tmp{os.getpid()}"
-        run(_link_binding(glue, tmp))
-        os.replace(tmp, BINDING_LIB)
+        if bound:
+            bound.result()
+            tmp = BINDING_LIB + f".tmp{os.getpid()}"
+            run(_link_binding(glue, tmp))
+            os.replace(tmp, BINDING_LIB)
+            os.makedirs(os.path.dirname(BINDING_STAMP), exist_ok=True)
+            with open(BINDING_STAMP, "w") as f:
+                f.write(stamp)
+        elif stamp is None:
+            print(f"no torch: {os.path.basename(BINDING_LIB)} is not built")
     return LIB
 
 
