@@ -72,7 +72,7 @@ int av_layer_norm(int64_t rows, int32_t n, int32_t dtype, int32_t param_dtype, f
     if (!in_rows(x, x_stride) || !out_rows(y, rows, n, y_stride) || !mean != !rstd)
         return AV_EINVAL;
     if (!aligned(x, type_bytes(dtype)) || !aligned(y, type_bytes(dtype)) || !aligned(weight, type_bytes(param_dtype)) ||
-        !aligned(bias, type_bytes(param_dtype)))
+        !aligned(bias, type_bytes(param_dtype)) || !aligned(mean, 4) || !aligned(rstd, 4))
         return AV_EINVAL;
     return status(launch_norm(rows, n, dtype, param_dtype, eps, x, x_stride, weight, bias, y, y_stride, mean, rstd,
                               as_stream(stream)));
@@ -89,7 +89,7 @@ int av_layer_norm_grad(int64_t rows, int32_t n, int32_t dtype, int32_t param_dty
     if (rows > 0 && (!in_rows(dy, dy_stride) || !in_rows(x, x_stride) || !mean || !rstd ||
                      !out_rows(dx, rows, n, dx_stride) || !aligned(dy, e) || !aligned(x, e) || !aligned(dx, e)))
         return AV_EINVAL;
-    if (!aligned(weight, pe) || !aligned(dweight, pe) || !aligned(dbias, pe))
+    if (!aligned(weight, pe) || !aligned(dweight, pe) || !aligned(dbias, pe) || !aligned(mean, 4) || !aligned(rstd, 4))
         return AV_EINVAL;
     const int64_t need = norm_work_bytes(rows, n);
     if (need > 0 && (!work || work_bytes < need || !aligned(work, 16)))

@@ -89,3 +89,17 @@ def test_the_binding_is_built_for_the_torch_that_is_there(tree):
     assert tree("1.0") == ([], True)
     assert tree("1.1") == (["g++", "g++"], True)
     assert tree("1.1") == ([], True)
+
+
+def test_statistics_off_their_alignment_are_refused():
+    """Like every other pointer of the operators: an address that is never read."""
+    import paper_2407_04221_gb300 as av
+    L, P = av.load(), 0x10000
+    ok = [4, 64, 1, 0, 1e-5, P, 64, P, P, P, 64, P, P, 0]
+    for k in (11, 12):  # mean, rstd
+        for bad in (P + 1, P + 2):
+            assert L.av_layer_norm(*ok[:k], bad, *ok[k + 1:]) == -1, k
+    ok = [4, 64, 1, 0, P, 64, P, 64, P, P, P, P, 64, P, P, P, 1 << 40, 0]
+    for k in (9, 10):
+        for bad in (P + 1, P + 2):
+            assert L.av_layer_norm_grad(*ok[:k], bad, *ok[k + 1:]) == -1, k
