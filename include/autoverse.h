@@ -382,7 +382,15 @@ int av_step_path(av_handle *h, int32_t *path);
  * input and no other output unless said otherwise.  Strides are in elements;
  * innermost axes are contiguous.  Every sum, softmax statistic and recurrent
  * state is held in 32 bits whatever the arrays' type, and no result depends on
- * the order in which blocks run: equal inputs give equal bits. */
+ * the order in which blocks run: equal inputs give equal bits.
+ *
+ * Kernels copy the aligned pieces of 16 bytes that hold an array's rows: up to
+ * 15 bytes before its first value and after its last are read too, and not used.
+ *
+ * A block waits for its own copies and products only, and each wait has a limit
+ * of some seconds.  Past it all that the block still writes is NaN, so that
+ * nothing wrong passes for right; the call has returned AV_OK long before, and
+ * the NaN are what tells of it. */
 enum { AV_F32 = 0, AV_BF16 = 1, AV_F16 = 2 }; /* value types, `dtype` below */
 
 /* Layer norm of rows x [rows][n] (row stride x_stride): mean and variance of
@@ -414,9 +422,7 @@ int av_layer_norm_work(int64_t rows, int32_t n, int64_t *bytes);
  * states: float [av_scan_sizes' states], kept for av_scan_grad, or NULL.
  * work: av_scan_sizes' work bytes, 16-byte aligned (may be NULL when 0).
  * Long sequences of few channels are cut into segments, whose inputs are read
- * twice; no block waits for another.  A block's wait for its own copies has a
- * limit of some seconds; past it the block writes NaN in place of its outputs,
- * so that no wrong state passes for a right one. */
+ * twice; no block waits for another. */
 int av_scan(int64_t T, int64_t B, int64_t D, int32_t dtype, const void *gate, int64_t gate_t,
             int64_t gate_b, const void *value, int64_t value_t, int64_t value_b,
             const uint8_t *reset, int64_t reset_t, int64_t reset_b, const float *h0, void *h,
@@ -462,7 +468,8 @@ int av_log_probs(int64_t rows, int32_t V, int32_t dtype, const void *logits, int
 /* Its gradient, from that of logp and of entropy (float [rows], each may be
  * NULL = 0) and what av_log_probs gave (entropy may be NULL with dentropy):
  *   dx_j = dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy),
- * 0 for entries masked and rows with nothing left.  dlogits has logits' type. */
+ * 0 for entries that are masked or of logit -inf and rows with nothing left.
+ * dlogits has logits' type. */
 int av_log_probs_grad(int64_t rows, int32_t V, int32_t dtype, const void *logits,
                       int64_t logit_stride, const void *tokens, int32_t token_bytes,
                       const uint8_t *mask, int64_t mask_stride, const float *dlogp,
@@ -475,7 +482,8 @@ int av_log_probs_grad(int64_t rows, int32_t V, int32_t dtype, const void *logits
  * D, H and the row strides are multiples of 8, rows apart (a stride is at least
  * the row's length), and the arrays 16-byte aligned: what TMA copies take.
  * act: AV_SILU, or AV_GELU (0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)))).
- * The products are exact and summed in 32 bits; h is rounded once. */
+ * The products are exact and summed in 32 bits; h is rounded once.  x may not be
+ * one row for all (its rows are apart), unlike the other operators' inputs. */
 enum { AV_SILU = 0, AV_GELU = 1 };
 int av_gated_ffn(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *x,
                  int64_t x_stride, const void *w, void *h, int64_t h_stride, uintptr_t stream);

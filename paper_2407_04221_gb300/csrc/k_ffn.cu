@@ -33,8 +33,10 @@ namespace {
 
 // ------------------------------------------------------------ activations
 
-// act(g) and its slope.  exp and the divide are the fast ones: good to 2^-21
-// relatively, a tenth of the outputs' rounding at most.
+// act(g) and its slope.  exp and the divide are the fast ones: the exponential is
+// good to 2 + 1.17 |g| units of 2^-23 (gelu: of the cubic), so the activation to
+// 2^-21 relatively near 0 and 2^-16 where it all but vanishes at |g| = 88, less
+// than a tenth of the outputs' rounding.
 template <int kAct>
 __device__ __forceinline__ void activate(float g, float &f, float &slope)
 {
@@ -98,7 +100,7 @@ __device__ __forceinline__ float scale_of(Peaks p)
 
 // The peaks, of finite values; they are zeroed before.  A warp takes a row, of dh,
 // x or w by the block's y; maxima do not depend on their order.  4,099 x 520 x
-// 1,368 7 us, 65,536 x 256 x 512 21, both from memory.
+// 1,368 some 8 us, 65,536 x 256 x 512 21, both from memory.
 template <class T>
 __global__ __launch_bounds__(kPeakThreads) void ffn_peaks_kernel(int64_t rows, int64_t D, int64_t H, const T *x, int64_t xs,
                                                                  const T *w, const T *dh, int64_t dhs, float4 *peaks)
@@ -421,9 +423,10 @@ __device__ __forceinline__ Tile tile_of(const Params &p, int i)
     return t;
 }
 
-// 16,384 x 1,024 x 4,096, bf16: h 160 us (1.72 PFLOP/s, tensor cores active 77 %
-// of the cycles, at the clock that power leaves), dg and du 193 (62 %: dh's loads
-// and the activations' gradients), dx 166 and dw 158 (93 %).
+// 16,384 x 1,024 x 4,096, bf16: h 156 us (1.76 PFLOP/s, tensor cores active 79 %
+// of the cycles, at the clock that power leaves), dg and du 243 (49 %: dh's loads,
+// the activations' gradients and the stores of two values), dx 319 and dw 310
+// (96 %), of two values twice the products.
 template <class T, int kForm, int kAct, bool kParts>
 __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) void ffn_kernel(
     const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,

@@ -417,7 +417,7 @@ struct Held {
 };
 
 // kLanes lanes a row of at most kLanes kPer entries, all in registers: 65,536
-// rows of 1,000 16-bit entries 45 us, with four alternatives 100; bound by issue.
+// rows of 1,000 16-bit entries 39 us, with four alternatives 98; bound by issue.
 template <class T, int kVec, int kLanes, int kPer, bool kTop>
 __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpArgs a, int top, float *logp,
                                                                      float *entropy, float *peak, float *logz,
@@ -570,7 +570,7 @@ __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_kernel(const LogpA
 }
 
 // A thread a row of at most kMost entries, all in registers: a million rows of
-// five 32-bit entries 16 us, with four alternatives 29.
+// five 32-bit entries 12 us, with four alternatives 26.
 template <class T, int kMost, bool kMask>
 __global__ __launch_bounds__(kTinyThreads) void logp_tiny_kernel(const LogpArgs a, int top, float *logp, float *entropy,
                                                                  float *peak, float *logz, float *top_logp,
@@ -706,7 +706,7 @@ __global__ __launch_bounds__(kNarrowThreads) void logp_narrow_grad_kernel(const 
 }
 
 // A block takes a part of a row, or a warp a row: 2,047 rows of 65,536 16-bit
-// entries 91 us, 5.9 TB/s; 20,000 of 2,000, by warps, 37 us, 4.3 TB/s.
+// entries 96 us, 5.6 TB/s; 20,000 of 2,000, by warps, 36 us, 4.4 TB/s.
 template <class T, int kLanes, bool kMask>
 __global__ __launch_bounds__(kGradThreads) void logp_wide_grad_kernel(const LogpArgs a, const float *dlogp,
                                                                       const float *dentropy, const float *peak,
@@ -761,8 +761,9 @@ __global__ __launch_bounds__(kGradThreads) void logp_wide_grad_kernel(const Logp
 
 // A thread a row.  The block's rows of 12 bytes or more, where they lie side by
 // side (kSide), go through shared memory, which lets neighbouring threads touch
-// neighbouring places: a million rows of seven 32-bit entries 25 us, straight 35,
-// of five 21 and 25, of seven 16-bit ones 23 and 27; of five 20 and 18.
+// neighbouring places: a million rows of seven 32-bit entries 21 us, straight 33,
+// of five 17 and 21, of seven 16-bit ones 18.5 and 25; of five, of ten bytes,
+// straight is the faster by a tenth, 16.5.
 template <class T, bool kMask, bool kSide>
 __global__ __launch_bounds__(kTinyThreads) void logp_grad_tiny_kernel(const LogpArgs a, const float *dlogp,
                                                                       const float *dentropy, const float *peak,
@@ -850,9 +851,9 @@ void with_lanes(int V, F f)
 bool small_blocks(int64_t rows, int64_t bytes) { return bytes <= 32768 && rows >= (bytes <= 16384 ? 608 : 1216); }
 
 // Whether a row's gradient takes a warp (else blocks, of 16,384 entries each):
-// 4,864 rows of 4,096 16-bit entries take 15 us by warps and 22 by blocks, 2,432
-// of 8,192 15.6 and 16.9, of 2,000 32-bit ones 9.0 and 10.7; but 608 of 1,500 6.7
-// and 5.6, 304 of 8,192 11.0 and 6.4, 2,432 of 8,192 32-bit ones 32 and 29.
+// 4,864 rows of 4,096 16-bit entries take 17 us by warps and 31 by blocks, 2,432
+// of 8,192 18.5 and 20.7, of 2,000 32-bit ones 10.3 and 12.4; but 304 of 8,192
+// 12.4 and 6.2, 2,432 of 8,192 32-bit ones 33 and 29; 608 of 1,500 6.2 either way.
 bool by_warps(int64_t rows, int64_t bytes) { return bytes <= 16384 && rows >= 1216; }
 
 // Rows of whole 16-byte packs.

@@ -513,7 +513,8 @@ __device__ __forceinline__ void put_pairs(T *out, int at, int wide, int n, int c
 }
 
 // Rows by bulk copies, up to kDeep a group ahead, whatever they start on: 65,536
-// rows of 1,024 16-bit values 43 us, 6.3 TB/s, at 2.5 of 4 instructions a cycle.
+// rows of 1,024 16-bit values 43 us alone, 6.3 TB/s, at 2.5 of 4 instructions a
+// cycle, and 55 one call after another, when the outputs before leave L2.
 template <class T, int kVec, int kPer, int kMost, int kMin>
 __global__ __launch_bounds__(kMost, kMin) void norm_ring_kernel(int64_t rows, int n, int size, float eps, const T *x,
                                                                 int64_t xs, const void *w, const void *b, int ptype,
@@ -620,7 +621,8 @@ __global__ __launch_bounds__(kMost, kMin) void norm_ring_kernel(int64_t rows, in
         linger();
 }
 
-// The same of x and dy: 74 us, 5.4 TB/s; warps wait at the groups' sums.
+// The same of x and dy: 74 us alone, 5.4 TB/s, and 80 one after another; warps
+// wait at the groups' sums.
 template <class T, int kVec, int kPer, int kMost, int kMin>
 __global__ __launch_bounds__(kMost, kMin) void norm_grad_ring_kernel(int64_t rows, int n, int size, const T *dy,
                                                                      int64_t dys, const T *x, int64_t xs,
@@ -771,7 +773,7 @@ __device__ float long_sum(float v, float *s)
 
 // A block a row, read three times, twice from L2 (counted down: the last step
 // up of a row of 2^31 - 1 values would go beyond an int): 1,500 rows of 20,011 16-bit
-// values 72 us, the gradient with the columns' sums 205.
+// values 79 us, the gradient with the columns' sums 202.
 template <class T>
 __global__ __launch_bounds__(kLongThreads) void norm_long_kernel(int64_t rows, int n, float eps, const T *x, int64_t xs,
                                                                  const void *w, const void *b, int ptype, T *y,

@@ -722,7 +722,7 @@ enum Way { kByTma, kByPairs, kBySingles };
 // 128 steps of 1,024 x 256 16-bit values take 60 us forward and 96 back, 3.4 and
 // 3.5 TB/s: two blocks of 128 registers a thread are resident, warps wait for
 // chunks half of the time and issue 1.9 and 1.7 of 4 instructions a cycle.
-// 65,537 steps of 1,021 32-bit channels, in segments, 287 and 489 us.
+// 65,537 steps of 1,021 32-bit channels, in segments, 304 and 504 us.
 template <class T, bool kBack, bool kMapsOnly, int kWay, int kRun>
 __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kBack, kRun)) void walk_kernel(
     const __grid_constant__ TensorMaps tma, const Args a)
@@ -1004,7 +1004,7 @@ struct Column {
 };
 
 // Sequences of at most kRun steps: a thread takes two channels.  Eight steps of
-// 4,096 x 64 16-bit values 16 us forward and 18 back (walked 39 and 53).
+// 4,096 x 64 16-bit values 13 us forward and 17 back (walked 39 and 53).
 template <class T, bool kBack, int kRun>
 __global__ __launch_bounds__(256) void brief_kernel(const Args a, bool pairs)
 {

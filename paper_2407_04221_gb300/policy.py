@@ -6,8 +6,13 @@ Argument marshalling only, as in the package itself: the functions make their
 outputs (torch, cuda), check what they are given (ValueError) and call the
 library's `av_*` function of the same name (in `csrc/policy_binding.cpp`), whose description in
 `include/autoverse.h` has the formulas and limits.  Nothing waits for the GPU.
-Arrays are float32, bfloat16 or float16; innermost axes are contiguous, the
-others may have any strides, inputs also those of broadcast (expanded) arrays.
+Arrays are float32, bfloat16 or float16 (the feed-forward's the latter two) and
+their innermost axes contiguous.  The axes before are taken together as rows,
+which are evenly spaced: whole arrays, parts of wider rows, every second row, one
+row expanded to many, but not two axes transposed.  The recurrence's steps and
+sequences have strides of their own, whatever they are.  The feed-forward takes
+rows that are apart, on 16 bytes and of a multiple of eight values, and its
+AvError (AV_EINVAL) says when they are not.
 
 Nothing is recorded by autograd: results are detached, and a call whose
 arguments require gradients warns of it where gradients are enabled.  Each
