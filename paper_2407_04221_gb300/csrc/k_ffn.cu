@@ -240,7 +240,7 @@ struct Params {
     int m, n;               // rows and columns of the result (forward forms: columns of H)
     int m_tiles, n_tiles;   // of a pair
     int k_blocks, splits;   // blocks of 64 terms in all, parts that they are dealt to
-    int k_once;             // of them those of A's first value; B's come again for the second
+    int k_once;             // of them those of A's second value, which come first; B's come again for the first
     const void *dh;
     int64_t dhs;
     Peaks peaks;            // what dg and du are scaled by, of float16
@@ -492,7 +492,8 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     if (rank == 0)
                         bar_expect(full + 8 * s, 4 * kHalf);
                     const uint32_t bar = in_cta(full + 8 * s, 0), a = base + s * 2 * kHalf, b = a + kHalf;
-                    const int second = !kGated && k >= p.k_once, term = (k - (second ? p.k_once : 0)) * kBlockK;
+                    // (what rounding left goes first: accumulators are truncated at every addition, small ones by little)
+                    const int second = !kGated && k < p.k_once, term = (k - (kGated || second ? 0 : p.k_once)) * kBlockK;
                     if (kARows) {
                         load_box(a, &a_map, am, term, second, bar);
                         load_box(a + kHalf / 2, &a_map, am + 64, term, second, bar);
