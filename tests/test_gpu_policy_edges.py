@@ -1,6 +1,6 @@
 """The policy operators at their edges: NaN among the alternatives of long rows, a state that is written where it was
 read, calls from two threads, rows of 2^31 - 1 values, arguments
-that require gradients."""
+that require gradients, gates of exactly zero."""
 from __future__ import annotations
 
 import ctypes
@@ -15,7 +15,7 @@ torch = pytest.importorskip("torch")
 from tests import test_gpu_policy_logp as logp  # noqa: E402
 from tests import test_gpu_policy_norm as norm  # noqa: E402
 from tests import test_gpu_policy_scan as scan  # noqa: E402
-from tests.policy_ref import BF16, F32, top_of  # noqa: E402
+from tests.policy_ref import BF16, F32, close, top_of  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -192,3 +192,25 @@ def test_detached_results_are_said(pol):
         assert torch.isfinite(wants.grad).all()
         with pytest.raises(UserWarning):
             calls[1]()
+
+
+@pytest.mark.parametrize("T,B,D,dtype", [(3, 80, 64, F32), (200, 2, 40, BF16), (3000, 1, 33, F32)])
+def test_gates_of_zero(pol, T, B, D, dtype):
+    """sigmoid(0) = 1/2 with a slope of 1/4: h_t = (h_{t-1} + v_t) / 2, dg_t = l_t (h_{t-1} - v_t) / 4, step by step in 64
+    bits; each of these operations is off by at most e of magnitudes below 8 in the kernel, and halves what was before."""
+    g, v, _, h0, dh, dlast = scan.make(T, B, D, dtype, None, T)
+    g.zero_()
+    h, last, states = pol.scan(g, v, None, h0, save=True)
+    dg, dv, dh0 = pol.scan_grad(dh, g, v, None, states, dlast=dlast)
+    before, state = [], h0.double().cpu()
+    for t in range(T):
+        before.append(state)
+        state = (state + v[t].double().cpu()) / 2
+    close(last, state, 8 * 16.0, "last")
+    flow = dlast.double().cpu()
+    for t in reversed(range(T)):
+        flow = flow + dh[t].double().cpu()
+        close(dv[t], flow / 2, 8 * 16.0, f"dv {t}")
+        close(dg[t], flow * (before[t] - v[t].double().cpu()) / 4, 64 * 16.0, f"dg {t}")
+        flow = flow / 2
+    close(dh0, flow, 8 * 16.0, "dh0")
