@@ -542,7 +542,9 @@ int av_head_log_probs(int64_t rows, int64_t D, int64_t V, int32_t dtype, const v
  *   G_rj = dlogp_r (1[j = token_r] - exp((l_rj - peak_r) - logz_r)),
  *   dx = G w,  dw = G^T x;
  * dx is 0 in rows without a token, which add nothing to dw.  The logits are made
- * again, a piece of the words at a time; G goes to the products as two values of
+ * again, summed as they were, a piece of the words at a time: of a row that is
+ * sure of its token, 1 - p is as exact as the forward pass's sum of exponentials
+ * (2^-24 at every addition).  G goes to the products as two values of
  * the arrays' type, the second what rounding the first leaves, so that only the
  * results are rounded.  Of AV_F16 it goes times a power of two that keeps the
  * largest in range.  work: the gradient's bytes of av_head_log_probs_work,

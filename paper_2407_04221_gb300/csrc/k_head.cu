@@ -40,11 +40,23 @@ struct Shared {
     float scale;
 };
 
-// A row's token and what its gradient takes: its slope is up (1[j = token] - exp2((l - m) log2(e) - zc)).
+// A row's token and what its gradient takes: its slope is up (1[j = token] - exp((l - m) - z)).
 struct Slope {
-    float m, zc, up;
+    float m, z, up;
     int token;
 };
+
+// 1 - exp(d).  Where that is small, by the series of (exp(d) - 1) / d, good to 0.5^10 / 11!; 8,192 x 256 x 32,768 with
+// the library's function 662 us, so 646.
+__device__ __forceinline__ float one_less_exp(float d)
+{
+    constexpr float kSeries[] = {1.0f / 3628800, 1.0f / 362880, 1.0f / 40320, 1.0f / 5040, 1.0f / 720, 1.0f / 120, 1.0f / 24, 1.0f / 6, 0.5f, 1.0f};
+    float sum = 0.0f;
+#pragma unroll
+    for (float c : kSeries)
+        sum = fmaf(sum, d, c);
+    return fabsf(d) < 0.5f ? -d * sum : 1.0f - exp2_fast(d * kLog2e);
+}
 
 // What brings the largest |G|, which is at most |dlogp|, below 2^15.
 __device__ __forceinline__ float scale_for(float top)
@@ -134,7 +146,7 @@ __global__ __launch_bounds__(kRowsThreads) void head_rows_kernel(int rows, int64
             if (token[k] >= 0) {
                 order[i] = (int)r;
                 if (kGrad)
-                    slopes[i] = {m[k], z[k] * kLog2e, up[k] * scale, token[k]};
+                    slopes[i] = {m[k], z[k], up[k] * scale, token[k]};
                 else
                     tokens[i] = token[k];
             } else if (!kGrad) {
@@ -219,7 +231,7 @@ __global__ __launch_bounds__(kOnceThreads) void head_once_kernel(int rows, int64
                 if (has) {
                     order[i] = r;
                     if (kGrad)
-                        slopes[i] = {peak[r], logz[r] * kLog2e, dlogp[r] * scale, (int)t};
+                        slopes[i] = {peak[r], logz[r], dlogp[r] * scale, (int)t};
                     else
                         tokens[i] = (int)t;
                 } else if (!kGrad) {
@@ -297,7 +309,7 @@ struct Params {
     const int *tokens;    // of the packed rows
     const Slope *slopes;
     float2 *parts;        // [tile of words][row]: maximum, sum
-    float *wanted;        // the token's logit
+    float *wanted;        // the tokens' logits (backward: those of few rows, summed as forward)
 };
 
 // A product's tiles.
@@ -310,12 +322,14 @@ struct Tile {
     int m, n, k0, k1, split;
 };
 
-// Blocks of 64 terms that accumulators take before they are added to sums in registers (forward).  The tensor cores
+// Blocks of 64 terms that accumulators take before they are added to sums in registers, of logits.  The tensor cores
 // truncate at every addition to the accumulator, a bias that grows with their number: of 8,192 x 1,024 x 65,536 the peaks
 // are off by 1.1e-6 of themselves, as root mean square, with all terms at once (616 us), by 5.2e-7 with eight blocks
-// (632), 2.5e-7 with four (670; sums in 32 bits 3.2e-7) and 1.3e-7 with two (783).  Backward the logits give shares of
-// 16 bits or 22.
+// (632), 2.5e-7 with four (670; sums in 32 bits 3.2e-7) and 1.3e-7 with two (783).  Backward they are the same sums, to the
+// last bit: m and logz are of them, and in a row that is sure of its token what is left of one, 1 - p, is of the size of
+// such errors (2.5 % of that call's gradient: 3.60 ms with all terms at once, 3.69 with these).
 constexpr int kPart = 4;
+__host__ __device__ constexpr int part_of(int form) { return of_logits(form) ? kPart : 1 << 30; }
 
 // Tiles in bands of eight rows of tiles, down the band first: those in flight together share A and B in L2.
 __device__ __forceinline__ Tile tile_of(const Work &p, int i)
@@ -504,7 +518,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                 const uint32_t kind = kind0 | (uint32_t)words << 15;
                 const int a_step = words ? 128 : 2;
                 for (int k0 = t.k0;;) {  // (a part may have no terms)
-                    const int k1 = kForm == kStats ? min(k0 + kPart, t.k1) : t.k1, set = done & 1;
+                    const int k1 = min(k0 + part_of(kForm), t.k1), set = done & 1;
                     if (!(ok = bar_wait(acc_empty + 8 * set, (done >> 1 & 1) ^ 1, dead)))
                         break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -571,7 +585,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                 wait_acc();
                 release(done++ & 1);  // (the next products may take them)
 #pragma unroll 1
-                for (int k = t.k0 + kPart; kForm == kStats && k < t.k1; k += kPart) {
+                for (int k = t.k0 + part_of(kForm); k < t.k1; k += part_of(kForm)) {
                     acc = part();
 #pragma unroll
                     for (int q = 0; q < 2 * kQ; ++q) {
@@ -639,9 +653,22 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     // rows would not be so small; the exponent's rounding is 2^-20 of the share then)
                     constexpr float kShift = 24.0f, kSmall = 1.0f / (1 << 24);
                     const float2 low = make_float2(-slope.m, -slope.m), c2 = make_float2(kLog2e, kLog2e),
-                                 zc = make_float2(kShift - slope.zc, kShift - slope.zc),
+                                 zc = make_float2(kShift - slope.z * kLog2e, kShift - slope.z * kLog2e),
                                  up = make_float2(-slope.up * kSmall, -slope.up * kSmall);
                     const int hit = slope.token - p.first - word0;  // of this team's words
+                    // the token's own: of a share near one the others are what is left, which the shifted exponent's rounding
+                    // would drown
+                    float own = 0.0f;
+                    if (hit >= 0 && hit < kCols) {
+#pragma unroll
+                        for (int q = 0; q < kQ; ++q)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                own = hit == q * 32 + e ? l[q][e] : own;
+                        if (p.wanted && ok)
+                            own = p.wanted[at];
+                        own = slope.up * one_less_exp((own - slope.m) - slope.z);
+                    }
 #pragma unroll
                     for (int q = 0; q < kQ; ++q) {
 #pragma unroll
@@ -654,8 +681,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                         if (hit >= q * 32 && hit < q * 32 + 32) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (hit == q * 32 + e)
-                                    l[q][e] = l[q][e] + slope.up;
+                                l[q][e] = hit == q * 32 + e ? own : l[q][e];
                         }
                         if (first)
                             stores_left<0>();
@@ -773,23 +799,16 @@ __device__ __forceinline__ void multiply_few(float (&c)[4], uint32_t a0, uint32_
         c[i] += p[i];
 }
 
-// A warp takes 16 words against up to eight rows of x, which stay in L1: the table's bytes stream past once, straight
-// into the operands of products of a warp (any order of the terms will do, as long as it is both's: a lane's 16 bytes
-// are eight terms of one word, and of x the same eight of one row).  Bound by the table's bytes: 4 x 1,024 x
-// 65,536 27 us with what follows, 5.0 TB/s (with half as many reads under way 29).
-template <class T>
-__global__ __launch_bounds__(kFewThreads, 7) void head_few_kernel(int rows, int64_t D, int64_t V, const T *x, int64_t xs, const T *w,
-                                                               const void *tokens, int token_bytes, float2 *parts, float *wanted)
+// The logits of 16 words, w0 and w1 a lane's, and up to eight rows of x, xr a lane's: a lane has words g and g + 8 of rows 2 t,
+// 2 t + 1, t the lane's number among four (any order of the terms will do, as long as it is both's: a lane's 16 bytes are
+// eight terms of one word, and of x the same eight of one row).  By whole warps: lanes whose terms are past the last go along
+// with zeros.
+template <class T, int kAhead>
+__device__ __forceinline__ void few_logits(float (&c)[4], const T *w0, const T *w1, const T *xr, int64_t D, int t)
 {
-    constexpr int kWarps = kFewThreads / 32, kAhead = 4;
-    __shared__ float2 of_warps[kWarps][kFewRows];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    next_may_start();
-    const int64_t j0 = ((int64_t)blockIdx.x * kWarps + warp) * 16;
-    const T *w0 = w + min(j0 + g, V - 1) * D, *w1 = w + min(j0 + g + 8, V - 1) * D, *xr = x + min(g, rows - 1) * xs;
-    float c[2][4] = {};
+    float sums[2][4] = {};
 #pragma unroll 1
-    for (int64_t k0 = 0; k0 < D; k0 += 32 * kAhead) {  // (whole warps: lanes whose terms are past the last go along with zeros)
+    for (int64_t k0 = 0; k0 < D; k0 += 32 * kAhead) {
         uint4 a[kAhead], b[kAhead], v[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -803,19 +822,36 @@ __global__ __launch_bounds__(kFewThreads, 7) void head_few_kernel(int rows, int6
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            multiply_few<T>(c[0], a[u].x, b[u].x, a[u].y, b[u].y, v[u].x, v[u].y);
-            multiply_few<T>(c[1], a[u].z, b[u].z, a[u].w, b[u].w, v[u].z, v[u].w);
+            multiply_few<T>(sums[0], a[u].x, b[u].x, a[u].y, b[u].y, v[u].x, v[u].y);
+            multiply_few<T>(sums[1], a[u].z, b[u].z, a[u].w, b[u].w, v[u].z, v[u].w);
         }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        c[0][i] += c[1][i];
+        c[i] = sums[0][i] + sums[1][i];
+}
+
+// A warp takes 16 words against up to eight rows of x, which stay in L1: the table's bytes stream past once, straight
+// into the operands of products of a warp.  Bound by the table's bytes: 4 x 1,024 x 65,536 27 us with what follows, 5.0
+// TB/s (with half as many reads under way 29).
+template <class T>
+__global__ __launch_bounds__(kFewThreads, 7) void head_few_kernel(int rows, int64_t D, int64_t V, const T *x, int64_t xs, const T *w,
+                                                               const void *tokens, int token_bytes, float2 *parts, float *wanted)
+{
+    constexpr int kWarps = kFewThreads / 32;
+    __shared__ float2 of_warps[kWarps][kFewRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    next_may_start();
+    const int64_t j0 = ((int64_t)blockIdx.x * kWarps + warp) * 16;
+    const T *w0 = w + min(j0 + g, V - 1) * D, *w1 = w + min(j0 + g + 8, V - 1) * D, *xr = x + min(g, rows - 1) * xs;
+    float c[4];
+    few_logits<T, 4>(c, w0, w1, xr, D, t);
     // a lane has words j0 + g, j0 + g + 8 of rows 2 t, 2 t + 1
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int r = 2 * t + i;
         const int64_t token = r < rows ? token_of(tokens, token_bytes, r) : -1;
-        const float l0 = j0 + g < V ? c[0][i] : no_value(), l1 = j0 + g + 8 < V ? c[0][2 + i] : no_value();
+        const float l0 = j0 + g < V ? c[i] : no_value(), l1 = j0 + g + 8 < V ? c[2 + i] : no_value();
         if (token >= 0 && token < V && (token == j0 + g || token == j0 + g + 8))
             wanted[r] = token == j0 + g ? l0 : l1;
         float m = fmaxf(fmaxf(l0, l1), kLowest);
@@ -839,6 +875,26 @@ __global__ __launch_bounds__(kFewThreads, 7) void head_few_kernel(int rows, int6
         }
         parts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = q;
     }
+}
+
+// Backward, a warp a row: the logit of its token as `head_few_kernel` has summed it, so that of a row whose token is the peak
+// l - m is 0.  (Of the tiles' sums it would be some 2^-21 of l, which of a confident row is more than what is left of one.)
+template <class T>
+__global__ __launch_bounds__(32, 1) void head_few_wanted_kernel(int rows, int64_t D, int64_t V, const T *x, int64_t xs, const T *w,
+                                                             const void *tokens, int token_bytes, float *wanted)
+{
+    const int lane = threadIdx.x, t = lane & 3, r = blockIdx.x;
+    next_may_start();
+    const int64_t each = lane < rows ? token_of(tokens, token_bytes, lane) : -1, token = __shfl_sync(~0u, each, r);
+    const int i = __popc(__ballot_sync(~0u, each >= 0 && each < V) & ((1u << r) - 1));  // of the packed rows
+    float c[4] = {};
+    if (token >= 0 && token < V) {
+        const T *of_token = w + token * D;
+        few_logits<T, 16>(c, of_token, of_token, x + min(lane >> 2, rows - 1) * xs, D, t);
+    }
+    after_previous();
+    if (token >= 0 && token < V && lane == r >> 1)
+        wanted[i] = c[r & 1];
 }
 
 // ------------------------------------------------------------ joining
@@ -1054,6 +1110,7 @@ Layout make_layout(int64_t rows, int64_t D, int64_t V, bool grad)
         return l;
     }
     l.slopes = take(rows * (int64_t)sizeof(Slope));
+    l.wanted = take(rows <= kFewRows ? rows * 4 : 0);
     l.piece = piece_of(rows, D, V);
     const int64_t words = l.piece < V ? l.piece : V;
     deal(rows, words, D, l.dx_splits, l.dw_splits);
@@ -1190,6 +1247,12 @@ cudaError_t launch_head_grad(const HeadArgs &a, const float *dlogp, const float 
         cudaError_t e = prepare_rows<true, kScaled<T>>(a, base, l, nullptr, const_cast<float *>(peak), const_cast<float *>(logz), dlogp, st);
         if (e != cudaSuccess)
             return e;
+        float *wanted = rows <= kFewRows ? reinterpret_cast<float *>(base + l.wanted) : nullptr;
+        if (wanted)
+            e = launch_chained(head_few_wanted_kernel<T>, rows, 32, 0, st, true, rows, a.D, a.V, (const T *)a.x,
+                               rows > 1 ? a.x_stride : a.D, (const T *)a.w, a.tokens, a.token_bytes, wanted);
+        if (e != cudaSuccess)
+            return e;
         float *sums = reinterpret_cast<float *>(base + l.dx), *dw_parts = reinterpret_cast<float *>(base + l.dw);
         CUtensorMap x, packed, xt, packedt, dx_map;
         const int64_t dx_dims[3] = {a.D, rows, l.dx_splits}, dx_strides[2] = {a.D, rows * a.D};
@@ -1225,6 +1288,7 @@ cudaError_t launch_head_grad(const HeadArgs &a, const float *dlogp, const float 
             p.more = j > 0;
             p.shared = shared;
             p.slopes = reinterpret_cast<const Slope *>(base + l.slopes);
+            p.wanted = wanted;
             e = go<T, kSlopes>(x, packed, wk, g, g, g_out, g_out, p, up(rows, kTile) * up(words, kTile), st);
             if (e != cudaSuccess)
                 return e;
