@@ -545,9 +545,11 @@ int av_head_log_probs(int64_t rows, int64_t D, int64_t V, int32_t dtype, const v
  * again, summed as they were, a piece of the words at a time: of a row that is
  * sure of its token, 1 - p is as exact as the forward pass's sum of exponentials
  * (2^-24 at every addition).  G goes to the products as two values of
- * the arrays' type, the second what rounding the first leaves, so that only the
- * results are rounded.  Of AV_F16 it goes times a power of two that keeps the
- * largest in range.  work: the gradient's bytes of av_head_log_probs_work,
+ * the arrays' type, the second what rounding the first leaves, and the products
+ * are summed in parts of 512 terms, which are added in 32 bits, so that only the
+ * results are rounded, however many rows and words there are.  Of AV_F16 G goes
+ * times a power of two that keeps the largest in range: values down to 2^-38 of
+ * the largest |dlogp| count.  work: the gradient's bytes of av_head_log_probs_work,
  * 256-byte aligned. */
 int av_head_log_probs_grad(int64_t rows, int64_t D, int64_t V, int32_t dtype, const float *dlogp,
                            const void *x, int64_t x_stride, const void *w, const void *tokens,

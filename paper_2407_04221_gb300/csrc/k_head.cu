@@ -329,7 +329,13 @@ struct Tile {
 // last bit: m and logz are of them, and in a row that is sure of its token what is left of one, 1 - p, is of the size of
 // such errors (2.5 % of that call's gradient: 3.60 ms with all terms at once, 3.69 with these).
 constexpr int kPart = 4;
-__host__ __device__ constexpr int part_of(int form) { return of_logits(form) ? kPart : 1 << 30; }
+
+// The same of the products.  At an addition sixteen products and the sum are truncated, together by some 2^-22.5 of it: sums
+// of one sign come out short.  With all terms at once, and with 32, 16, 8 and 4 blocks: dw of 262,144 rows by 8.3e-4, 1.2e-5,
+// 5.1e-6, 1.9e-6 and 4e-7 of itself, dx of 100,000 words by 3.5e-4, 1.2e-5, 5.9e-6, 2.8e-6 and 1.3e-6 (float16's largest
+// rounding is 4.9e-4); the gradient of 8,192 x 1,024 x 65,536 takes 3.69, 3.80, 3.79, 3.84 and 3.94 ms.
+constexpr int kSumPart = 8;
+__host__ __device__ constexpr int part_of(int form) { return of_logits(form) ? kPart : kSumPart; }
 
 // Tiles in bands of eight rows of tiles, down the band first: those in flight together share A and B in L2.
 __device__ __forceinline__ Tile tile_of(const Work &p, int i)
@@ -492,7 +498,7 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                         load_box(b, &w_map, k * kBlockK, bn, bar);
                         continue;
                     }
-                    // (what rounding left goes first: accumulators are truncated at every addition, small ones by little)
+                    // (what rounding left goes first, and so into sums of its own but for one part)
                     const int second = k < work.k_once, term = (k - (second ? 0 : work.k_once)) * kBlockK;
                     if (words) {
                         load_box(a, &across_map, am, term, second, bar);
@@ -699,31 +705,48 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     }
                 }
             } else {
-                const int set = done & 1;
-                ok = __all_sync(~0u, ok && bar_wait(acc_full + 8 * set, done >> 1 & 1, dead));
-                ++done;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t acc = tmem + set * kTile + ((uint32_t)(quarter * 32) << 16);
-                const float other = ok ? 0.0f : __int_as_float(0x7fffffff);  // (a part may have no terms)
-                const bool products = ok && t.k0 < t.k1;
-                auto columns = [&](int c, float (&v)[32]) {
-                    if (products) {
-                        load_acc(acc + c, v);
-                    } else {
+                // this team's columns, summed over the parts of their terms
+                float v[kQ][32];
+                auto part = [&] {  // where the next is
+                    const int set = done & 1;
+                    ok = __all_sync(~0u, ok && bar_wait(acc_full + 8 * set, done >> 1 & 1, dead));
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    return tmem + set * kTile + ((uint32_t)(quarter * 32) << 16) + team * kCols;
+                };
+                uint32_t acc = part();
+#pragma unroll
+                for (int q = 0; q < kQ; ++q)
+                    load_acc(acc + q * 32, v[q]);
+                wait_acc();
+                release(done++ & 1);  // (the next products may take them)
+#pragma unroll 1
+                for (int k = t.k0 + part_of(kForm); k < t.k1; k += part_of(kForm)) {
+                    acc = part();
+#pragma unroll
+                    for (int q = 0; q < 2 * kQ; ++q) {
+                        float u[16];
+                        load_acc(acc + q * 16, u);
+                        wait_acc();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            v[q >> 1][(q & 1) * 16 + e] += u[e];
+                    }
+                    release(done++ & 1);
+                }
+                if (!ok || t.k0 >= t.k1) {  // (a part may have no terms)
+                    const float other = ok ? 0.0f : __int_as_float(0x7fffffff);
+#pragma unroll
+                    for (int q = 0; q < kQ; ++q)
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            v[e] = other;
-                    }
-                };
-                // this team's columns: 16-bit results 64 at a time, sums in 32 bits 32
+                            v[q][e] = other;
+                }
+                // 16-bit results go 64 columns at a time, sums in 32 bits 32
                 const bool parts = !words || p.dw_splits > 1;
                 const CUtensorMap *out = words ? &dw_map : &out_map;
 #pragma unroll
                 for (int q = 0; q < kQ; ++q) {
                     const bool half = q & 1;
-                    float v[32];
-                    columns(team * kCols + q * 32, v);
-                    wait_acc();
                     if (parts || !half) {
                         if (first)
                             stores_left<0>();
@@ -732,15 +755,15 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     if (parts) {
 #pragma unroll
                         for (int c = 0; c < 8; ++c)
-                            put16(slab0, row, c, __float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
-                                  __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+                            put16(slab0, row, c, __float_as_uint(v[q][4 * c]), __float_as_uint(v[q][4 * c + 1]),
+                                  __float_as_uint(v[q][4 * c + 2]), __float_as_uint(v[q][4 * c + 3]));
                     } else {
                         if (kScaled<T>) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                v[e] *= back;
+                                v[q][e] *= back;
                         }
-                        put32<T>(slab0, row, half, v);
+                        put32<T>(slab0, row, half, v[q]);
                     }
                     if (!parts && !half)
                         continue;
@@ -756,7 +779,6 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                     if (first)
                         stores_close();
                 }
-                release(set);
             }
         }
         if (first)

@@ -1,4 +1,4 @@
-"""What the sums of the head's gradient leave of terms that cancel: those of rows that are sure of their token."""
+"""What the sums of the head's gradient leave: long ones, and those in which a confident row's terms cancel."""
 from __future__ import annotations
 
 import pytest
@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from tests.policy_ref import BF16, E, F16, ROUNDOFF  # noqa: E402
-from tests.test_gpu_policy_head import definition  # noqa: E402
+from tests.test_gpu_policy_head import definition, make  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -17,6 +17,49 @@ def pol():
         pytest.skip("no CUDA device")
     from paper_2407_04221_gb300 import policy
     return policy
+
+
+def one_sign(rows, D, V, dtype):
+    """Positive x and w, of which columns, rows and words are of different sizes, so that results lie anywhere between two
+    values of the type.  All tokens are word 0, whose row of w is 0: of the others G has one sign."""
+    gen = torch.Generator(device="cuda").manual_seed(rows + V)
+    uniform = lambda *shape: torch.rand(*shape, generator=gen, device="cuda")  # noqa: E731
+    column = 2.0**uniform(D)
+    x = ((0.5 + uniform(rows, D)) * column * 2.0**uniform(rows, 1) / 4).to(dtype)
+    w = (uniform(V, D) * column * 6 * uniform(V, 1) / D).to(dtype)
+    w[0] = 0
+    return x, w, torch.zeros(rows, dtype=torch.int64, device="cuda"), -torch.ones(rows, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,D,V", [(262144, 1024, 1024), (64, 4096, 100000)])
+def test_long_sums_of_one_sign(pol, rows, D, V, dtype):
+    """Terms of one sign: 262,144 of dw, 100,000 of dx.  At an addition a tensor core truncates sixteen products and the sum,
+    together by some 2^-22.5 of the sum; one that grows evenly is half its last on average.  Of 512 terms, 32 additions,
+    that is 2^-18.5 of the result; sums of those are rounded.  The mean error of N results beside it is that of their
+    rounding, at most u each, (u / 3^1/2) / N^1/2 as root mean square, of which four are allowed, and 2^-20 for
+    exponentials whose errors have one sign."""
+    x, w, tok, dl = one_sign(rows, D, V, dtype)
+    grads = pol.head_log_probs_grad(dl, x, w, tok, pol.head_log_probs(x, w, tok))
+    want = definition(x, w, tok, dl)[1:3]
+    for name, got, exact in zip(("dx", "dw"), grads, (want[0], want[1])):
+        if name == "dw":
+            got, exact = got[1:], exact[1:]
+        off = float(((got.double() - exact) / exact).mean())
+        assert abs(off) <= 2.0**-18 + 2.0**-20 + 4 * ROUNDOFF[dtype] / (3 * got.numel())**0.5, (name, off)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,D,V", [(300, 4096, 1500), (60000, 64, 520), (8200, 1024, 4100)])
+def test_gradient_of_many_terms_is_as_exact_as_rounding_once(pol, rows, D, V, dtype):
+    """As `test_gradient_is_as_exact_as_rounding_once`, of more terms: those of a sum that is truncated are 512 at most, less
+    than 2^-17 of the result, and logits of D terms are made of parts of 256, whose truncation leaves
+    2^-20 of |l| < 16 in the shares: 2^-16, 0.1 of float16's 0.3 x 2^-11; 1.005 in quadrature.  1.02 is allowed."""
+    x, w, tok, dl = make(rows, D, V, dtype, rows + V)
+    want = definition(x, w, tok, dl)[1:3]
+    for name, got, exact in zip(("dx", "dw"), pol.head_log_probs_grad(dl, x, w, tok, pol.head_log_probs(x, w, tok)), want):
+        off, once = (float((v.double() - exact).norm()) for v in (got, exact.to(dtype)))
+        assert off <= 1.02 * once, (name, off / once)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
