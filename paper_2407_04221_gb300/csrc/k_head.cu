@@ -689,6 +689,12 @@ __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) voi
                             for (int e = 0; e < 32; ++e)
                                 l[q][e] = hit == q * 32 + e ? own : l[q][e];
                         }
+                        // (rows past the last: x is 0 there, and 0 times what w holds may be NaN)
+                        if (m0 + quarter * 32 + 32 > count) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                l[q][e] = here ? l[q][e] : 0.0f;
+                        }
                         if (first)
                             stores_left<0>();
                         team_sync(team);

@@ -1,0 +1,53 @@
+"""What is not finite in the operators over cell words: in tables, logits, teachers, and places that do not count."""
+from __future__ import annotations
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests.policy_ref import BF16, F16  # noqa: E402
+from tests.test_gpu_policy_head import make  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+NAN, INF = math.nan, math.inf
+
+
+@pytest.fixture(scope="module")
+def pol():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2407_04221_gb300 import policy
+    return policy
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [1, 7, 40, 256, 700])
+def test_head_without_tokens(pol, rows, dtype):
+    """Rows without a token add nothing to dw, whatever the table holds."""
+    x, w, tok, dl = make(rows, 72, 500, dtype, rows)
+    w[3], w[77, 5], w[499] = NAN, INF, -INF
+    tok[:] = -1
+    out = pol.head_log_probs(x, w, tok)
+    assert not any(out[k].any() for k in out)
+    dx, dw = pol.head_log_probs_grad(dl, x, w, tok, out)
+    assert not dx.any() and not dw.any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("count", [1, 3, 63, 64, 65, 200, 256, 300])
+@pytest.mark.parametrize("absent", [0, 90])
+def test_head_word_that_nothing_says(pol, count, absent, dtype):
+    """A word of logit -inf in all rows: its share and its row of dw are 0, of any number of rows, with padding or without."""
+    x, w, tok, dl = make(count + absent, 72, 500, dtype, count, 0.0)
+    tok[count:] = -1
+    x, tok = (v[torch.randperm(count + absent, generator=torch.Generator().manual_seed(count)).cuda()] for v in (x, tok))
+    x[:, 5] = x[:, 5].abs() + 0.5
+    tok[tok == 77] = 78
+    w[77, 5] = -INF
+    out = pol.head_log_probs(x, w, tok)
+    assert all(torch.isfinite(out[k]).all() for k in out)
+    _, dw = pol.head_log_probs_grad(dl, x, w, tok, out)
+    assert not dw[77].any()
+    assert torch.isfinite(dw).all()
