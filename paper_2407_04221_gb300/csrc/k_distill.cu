@@ -302,12 +302,12 @@ __global__ __launch_bounds__(kTinyThreads) void distill_tiny_kernel(const Distil
 // What a row's gradient takes: p = exp2((x - m) c - zc), times up; nothing where it is not live.
 struct Slope {
     float m, c, zc, up;
-    bool live, plain;  // plain: a share of 0 makes a gradient of 0
+    bool live, plain;  // plain: an entry of -inf makes a gradient of 0
 };
 __device__ __forceinline__ Slope slope_of(const DistillArgs &a, int64_t r, const float *dkl, const float *peak, const float *logz)
 {
     const float z = logz[r], up = dkl[r] * a.inv;
-    return {peak[r], a.inv * kLog2e, z * kLog2e, up, z != no_value(), fabsf(up) <= 3.402823466e38f};
+    return {peak[r], a.inv * kLog2e, z * kLog2e, up, z != no_value(), fabsf(up) <= 3.402823466e38f && fabsf(z) <= 3.402823466e38f};
 }
 __device__ __forceinline__ float share(const Slope &s, float x) { return exp2_whole(fmaf(x - s.m, s.c, -s.zc)); }
 

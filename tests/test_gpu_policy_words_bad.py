@@ -7,7 +7,8 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from tests.policy_ref import BF16, F16  # noqa: E402
+from tests import test_gpu_policy_distill as dis  # noqa: E402
+from tests.policy_ref import BF16, F16, F32  # noqa: E402
 from tests.test_gpu_policy_head import make  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -51,3 +52,34 @@ def test_head_word_that_nothing_says(pol, count, absent, dtype):
     _, dw = pol.head_log_probs_grad(dl, x, w, tok, out)
     assert not dw[77].any()
     assert torch.isfinite(dw).all()
+
+
+SIZES = [5, 8, 9, 100, 1000, 1500, 5000, 33001]
+
+
+def at_start(x, start):
+    """The same rows, from elsewhere in 16 bytes."""
+    wide = torch.zeros(x.shape[0], x.shape[1] + 9, dtype=x.dtype, device=x.device)
+    wide[:, start:start + x.shape[1]] = x
+    return wide[:, start:start + x.shape[1]]
+
+
+@pytest.mark.parametrize("V", SIZES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("start", [0, 1])
+def test_distill_entries_that_are_not_there(pol, V, dtype, start):
+    """Masked entries and those of logit -inf have no gradient, whatever else their row holds: NaN, +inf."""
+    x, t, index, m, dkl = dis.make(1300 if V == 1500 else 40, V, 4, dtype, V, True, 0.0)
+    x = at_start(x, start)
+    x[:, 1::5], m[:, 2::7] = -INF, 0
+    m[:, 0], x[:, 0] = 1, 1.0
+    x[1, 0], x[3, 0], x[5, V - 1] = NAN, INF, NAN
+    m[5, V - 1] = 1
+    out = pol.distill(x, t, index, mask=m)
+    got = pol.distill_grad(dkl, x, t, index, out, mask=m)
+    gone = (m == 0) | (x == -INF)
+    assert not got[gone].any()
+    for r in (1, 3, 5):
+        assert torch.isnan(got[r][~gone[r]]).all() and torch.isnan(out["kl"][r])
+    keep = torch.isfinite(out["logz"])
+    assert int(keep.sum()) == x.shape[0] - 3 and torch.isfinite(got[keep]).all()
