@@ -548,14 +548,14 @@ __global__ __launch_bounds__(kTinyThreads) void distill_tiny_grad_kernel(const D
     int at[kTiny];
     float t[kTiny], w[kTiny], top = no_value(), sum = 0.0f;
     taught_all(a, r, at, t);
-    bool some = false;
+    uint32_t named = 0;  // bits of entries
 #pragma unroll
     for (int i = 0; i < kTiny; ++i) {
-        some |= at[i] >= 0;
+        named |= at[i] >= 0 ? 1u << at[i] : 0;
         top = fmaxf(top, t[i]);
         w[i] = 0.0f;
     }
-    s.live &= some;
+    s.live &= named != 0;
 #pragma unroll
     for (int i = 0; i < kTiny; ++i) {
         if (i >= a.k)
@@ -573,7 +573,8 @@ __global__ __launch_bounds__(kTinyThreads) void distill_tiny_grad_kernel(const D
         if (j >= a.V)
             break;
         const float v = kMask && mask[j] == 0 ? no_value() : to_f32(x[j]);
-        dx[j] = from_f32<T>(s.live && v != no_value() ? (share(s, v) - w[j] * part) * s.up : 0.0f);
+        const float taken = named >> j & 1 ? w[j] * part : 0.0f;  // (part may be NaN)
+        dx[j] = from_f32<T>(s.live && v != no_value() ? (share(s, v) - taken) * s.up : 0.0f);
     }
 }
 

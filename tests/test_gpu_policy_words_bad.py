@@ -83,3 +83,21 @@ def test_distill_entries_that_are_not_there(pol, V, dtype, start):
         assert torch.isnan(got[r][~gone[r]]).all() and torch.isnan(out["kl"][r])
     keep = torch.isfinite(out["logz"])
     assert int(keep.sum()) == x.shape[0] - 3 and torch.isfinite(got[keep]).all()
+
+
+@pytest.mark.parametrize("V", SIZES)
+@pytest.mark.parametrize("bad", [NAN, INF])
+def test_distill_bad_teachers(pol, V, bad):
+    """A teacher's value that is NaN or +inf makes kl NaN, and the gradient of the entries that the row's alternatives name;
+    the others have their share of it, as without a teacher's weight."""
+    x, t, index, m, dkl = dis.make(1300 if V == 1500 else 40, V, 3, F32, V, gone=0.0)
+    good = pol.distill(x, t, index)
+    right = pol.distill_grad(dkl, x, t, index, good)
+    t[1, 2], t[4, 0] = bad, bad
+    out = pol.distill(x, t, index)
+    got = pol.distill_grad(dkl, x, t, index, out)
+    named = torch.zeros_like(x, dtype=torch.bool).scatter_(1, index.long(), True)
+    bad_rows = torch.zeros_like(named[:, 0])
+    bad_rows[[1, 4]] = True
+    assert torch.equal(torch.isnan(out["kl"]), bad_rows) and torch.equal(torch.isnan(got), named & bad_rows[:, None])
+    assert torch.equal(got[~(named & bad_rows[:, None])], right[~(named & bad_rows[:, None])])
