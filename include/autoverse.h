@@ -570,7 +570,8 @@ int av_head_log_probs_work(int64_t rows, int64_t D, int64_t V, int64_t *forward,
  * float [rows] each (peak and logz may be NULL).  An alternative whose index is
  * outside 0..V-1 or whose value is -inf is not there; with none left kl is 0.  An
  * index that comes twice counts twice.  mask: as av_log_probs'.  An alternative of
- * weight above 0 that is masked or of logit -inf makes kl +inf; NaN or +inf among
+ * weight above 0 (exp of 32 bits: down to 2^-149 of the largest) that is masked or
+ * of logit -inf makes kl +inf; NaN or +inf among
  * what is there makes it NaN. */
 int av_distill(int64_t rows, int32_t V, int32_t dtype, const void *logits, int64_t logit_stride,
                const void *teacher, int32_t teacher_dtype, const void *index, int32_t index_bytes,

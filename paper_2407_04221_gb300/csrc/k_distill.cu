@@ -85,9 +85,9 @@ __device__ __forceinline__ float divergence(const DistillArgs &a, int64_t r, boo
     auto weigh_in = [&](int j, float t) {
         if (j < 0)
             return;
-        const float d = (t - top) * a.inv, e = exp2_fast(d * kLog2e);
+        const float d = (t - top) * a.inv, e = exp2_whole(d * kLog2e);
         sum += e;
-        if (e != 0.0f)  // (an alternative of no weight may be one that the student does not have)
+        if (e != 0.0f)  // (an alternative of no weight, below 2^-149, may be one that the student does not have)
             mix += e * (d - (x(j) - m) * a.inv);
     };
     if (kAhead)
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(kTinyThreads) void distill_tiny_kernel(const Distil
             break;
         if (at[i] < 0)
             continue;
-        const float d = (t[i] - top) * a.inv, w = exp2_fast(d * kLog2e);
+        const float d = (t[i] - top) * a.inv, w = exp2_whole(d * kLog2e);
         sum += w;
         if (w != 0.0f) {
             const float low = kMask && mask[at[i]] == 0 ? no_value() : to_f32(x[at[i]]);
@@ -354,7 +354,7 @@ __device__ __forceinline__ bool weigh(const DistillArgs &a, int64_t r, bool here
     top = lanes_max<kLanes>(top);
     float sum = 0.0f;
     for (int i = lane; here && i < a.k; i += kLanes) {
-        const float e = at[i] >= 0 ? exp2_fast((weight[i] - top) * a.inv * kLog2e) : 0.0f;
+        const float e = at[i] >= 0 ? exp2_whole((weight[i] - top) * a.inv * kLog2e) : 0.0f;
         weight[i] = e;
         sum += e;
     }
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(kTinyThreads) void distill_tiny_grad_kernel(const D
     for (int i = 0; i < kTiny; ++i) {
         if (i >= a.k)
             break;
-        const float e = at[i] >= 0 ? exp2_fast((t[i] - top) * a.inv * kLog2e) : 0.0f;
+        const float e = at[i] >= 0 ? exp2_whole((t[i] - top) * a.inv * kLog2e) : 0.0f;
         sum += e;
 #pragma unroll
         for (int j = 0; j < kTiny; ++j)

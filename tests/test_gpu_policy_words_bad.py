@@ -101,3 +101,18 @@ def test_distill_bad_teachers(pol, V, bad):
     bad_rows[[1, 4]] = True
     assert torch.equal(torch.isnan(out["kl"]), bad_rows) and torch.equal(torch.isnan(got), named & bad_rows[:, None])
     assert torch.equal(got[~(named & bad_rows[:, None])], right[~(named & bad_rows[:, None])])
+
+
+@pytest.mark.parametrize("V", SIZES)
+@pytest.mark.parametrize("heat", [1.0, 2.0])
+def test_distill_weights_of_almost_nothing(pol, V, heat):
+    """An alternative whose weight is above 0 in 32 bits, down to 2^-149, and that the student does not have makes kl
+    infinite; one whose weight is 0 there does not."""
+    x, t, index, _, dkl = dis.make(8, V, 2, F32, V, gone=0.0)
+    index[:, 0], index[:, 1] = 0, 2
+    below = torch.tensor([0.0, 20.0, 80.0, 88.0, 95.0, 102.0, 110.0, 1000.0], device="cuda") * heat
+    t[:, 0], t[:, 1] = 3.0, 3.0 - below
+    m = torch.ones(V, dtype=torch.uint8, device="cuda")
+    m[2] = 0
+    kl = pol.distill(x, t, index, temperature=heat, mask=m)["kl"]
+    assert torch.isinf(kl[:6]).all() and torch.isfinite(kl[6:]).all()
