@@ -526,8 +526,8 @@ int av_embed_work(int64_t rows, int64_t V, int64_t D, int64_t *bytes);
  * [V][D] (contiguous) of type AV_BF16 or AV_F16; the logits are kept nowhere.
  * peak = max l, logz = log sum exp(l - peak), logp = (l_token - peak) - logz
  * (float [rows]; peak and logz may be NULL), as av_log_probs defines them; NaN
- * among a row's logits makes all three NaN.  A row
- * without a token is not looked at: its x may hold anything and its results are 0.
+ * or +inf among a row's logits makes logz and logp NaN, and peak +inf where one is,
+ * else NaN.  A row without a token is not looked at: its x may hold anything and its results are 0.
  * D and the row strides are multiples of 8, rows apart, arrays 16-byte aligned;
  * V is any; rows, V, D < 2^30 and (rows / 256) (V / 256) < 2^30, rounded up.
  * Products are exact and summed in 32 bits.
@@ -571,8 +571,8 @@ int av_head_log_probs_work(int64_t rows, int64_t D, int64_t V, int64_t *forward,
  * outside 0..V-1 or whose value is -inf is not there; with none left kl is 0.  An
  * index that comes twice counts twice.  mask: as av_log_probs'.  An alternative of
  * weight above 0 (exp of 32 bits: down to 2^-149 of the largest) that is masked or
- * of logit -inf makes kl +inf; NaN or +inf among
- * what is there makes it NaN. */
+ * of logit -inf makes kl +inf; NaN or +inf among what is there makes it
+ * NaN.  Of the logits it makes logz NaN, and peak +inf where one is, else NaN. */
 int av_distill(int64_t rows, int32_t V, int32_t dtype, const void *logits, int64_t logit_stride,
                const void *teacher, int32_t teacher_dtype, const void *index, int32_t index_bytes,
                int32_t k, float temperature, const uint8_t *mask, int64_t mask_stride, float *kl,

@@ -140,7 +140,7 @@ __device__ __forceinline__ void leave(const DistillOut &o, int64_t r, float kl, 
 {
     o.kl[r] = kl;
     if (o.peak)
-        o.peak[r] = z == no_value() ? no_value() : m;
+        o.peak[r] = z == no_value() || (z != z && m != INFINITY) ? z : m;  // (NaN has not been compared)
     if (o.logz)
         o.logz[r] = z;
 }

@@ -934,7 +934,7 @@ __device__ __forceinline__ void leave(int64_t r, bool has, float2 q, const float
     const float z = q.y != 0.0f ? logf(q.y) : no_value();  // (NaN counts)
     logp[r] = !has ? 0.0f : z == no_value() ? z : (*wanted - q.x) - z;
     if (peak)
-        peak[r] = !has ? 0.0f : z == no_value() || z != z ? z : q.x;  // (NaN has not been compared)
+        peak[r] = !has ? 0.0f : z == no_value() || (z != z && q.x != INFINITY) ? z : q.x;  // (NaN has not been compared)
     if (logz)
         logz[r] = has ? z : 0.0f;
 }

@@ -54,6 +54,21 @@ def test_head_word_that_nothing_says(pol, count, absent, dtype):
     assert torch.isfinite(dw).all()
 
 
+@pytest.mark.parametrize("bad", [NAN, INF])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_head_peaks(pol, rows, bad):
+    """The largest logit: infinite where one is, else NaN where one is; both make logz and logp NaN."""
+    x, w, tok, _ = make(rows, 64, 300, BF16, rows, 0.0)
+    good = pol.head_log_probs(x, w, tok)
+    x = x.abs() + 0.5
+    w[7] = 0
+    w[7, 3] = bad
+    tok[tok == 7] = 8
+    out = pol.head_log_probs(x, w, tok)
+    assert torch.isnan(out["logz"]).all() and torch.isnan(out["logp"]).all()
+    assert torch.equal(out["peak"].nan_to_num(1.0, 2.0, 3.0), torch.full_like(good["peak"], bad).nan_to_num(1.0, 2.0, 3.0))
+
+
 SIZES = [5, 8, 9, 100, 1000, 1500, 5000, 33001]
 
 
@@ -66,11 +81,11 @@ def at_start(x, start):
 
 @pytest.mark.parametrize("V", SIZES)
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("start", [0, 1])
+@pytest.mark.parametrize("start", [None, 0, 1])
 def test_distill_entries_that_are_not_there(pol, V, dtype, start):
     """Masked entries and those of logit -inf have no gradient, whatever else their row holds: NaN, +inf."""
     x, t, index, m, dkl = dis.make(1300 if V == 1500 else 40, V, 4, dtype, V, True, 0.0)
-    x = at_start(x, start)
+    x = x if start is None else at_start(x, start)
     x[:, 1::5], m[:, 2::7] = -INF, 0
     m[:, 0], x[:, 0] = 1, 1.0
     x[1, 0], x[3, 0], x[5, V - 1] = NAN, INF, NAN
@@ -116,3 +131,16 @@ def test_distill_weights_of_almost_nothing(pol, V, heat):
     m[2] = 0
     kl = pol.distill(x, t, index, temperature=heat, mask=m)["kl"]
     assert torch.isinf(kl[:6]).all() and torch.isfinite(kl[6:]).all()
+
+
+@pytest.mark.parametrize("V", SIZES)
+def test_distill_peaks(pol, V):
+    """As the head's: infinite where a logit is, else NaN where one is, -inf where nothing is left."""
+    x, t, index, _, _ = dis.make(40, V, 2, F32, V, gone=0.0)
+    x[1, 2], x[3, 0], x[5], x[7, 1] = NAN, INF, -INF, -INF
+    x[9, 1], x[9, 4] = NAN, INF
+    out = pol.distill(x, t, index)
+    want = x.amax(1)
+    want[9] = INF
+    assert torch.equal(out["peak"].nan_to_num(9.0, 1e30, -1e30), want.nan_to_num(9.0, 1e30, -1e30))
+    assert torch.equal(torch.isnan(out["logz"]), torch.isnan(x).any(1) | (x == INF).any(1))
