@@ -564,7 +564,8 @@ int av_head_log_probs_work(int64_t rows, int64_t D, int64_t V, int64_t *forward,
  * alternatives (1..min(V, AV_MAX_TEACHER)): teacher [rows][k] of teacher_dtype,
  * logits or log probabilities (a constant added to a row changes nothing), index
  * [rows][k] of index_bytes 4 (int32) or 8 (int64), both contiguous; for instance
- * av_log_probs' alternatives.  With x the row's logits / temperature,
+ * av_log_probs' alternatives.  temperature: from 2^-126 to 3e38.  With x the row's
+ * logits / temperature,
  *   peak = max of the logits,  logz = log sum exp(x - peak / temperature),
  *   q = softmax(teacher / temperature),  kl = sum q_i (log q_i - log p_{index_i}),
  * float [rows] each (peak and logz may be NULL).  An alternative whose index is

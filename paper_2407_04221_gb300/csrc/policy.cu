@@ -304,7 +304,7 @@ bool distill_ok(int64_t rows, int32_t V, int32_t dtype, const void *logits, int6
 {
     if (V < 1 || !size_ok(rows, V) || rows > (int64_t(1) << 31) - 1 || !type_ok(dtype) || !type_ok(teacher_dtype) ||
         (index_bytes != 4 && index_bytes != 8) || k < 1 || k > AV_MAX_TEACHER || k > V || !(temperature > 0.0f) ||
-        !(temperature <= 3.0e38f) || !(1.0f / temperature <= 3.0e38f))
+        !(temperature <= 3.0e38f) || !(1.0f / temperature <= 1.0e38f))  // (times log2(e) it is finite too)
         return false;
     if (rows == 0)
         return true;

@@ -84,3 +84,13 @@ def test_binding_refuses_what_it_cannot_pass():
                  lambda: pol.distill_grad(x[:, 0], x, x, tok, dict(peak=None, logz=None)), lambda: pol.embed(tok, x, stream=5)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("temperature", [1.5e-39, 3.4e-39, 4.9e-39])
+def test_distill_temperatures_too_low(lib, temperature):
+    """1 / temperature times log2(e) has to be finite: else the peak would be 0 times infinity."""
+    forward = [4, 100, 1, P, 100, P, 0, P, 4, 8, temperature, None, 0, P, P, P, 0]
+    assert lib.av_distill(*forward) == -1
+    assert lib.av_distill_grad(*forward[:13], P, P, P, P, 100, 0) == -1
+    ok = [0, 100, 1, None, 100, None, 0, None, 4, 8, 2.0**-126, None, 0, None, None, None, 0]
+    assert lib.av_distill(*ok) == 0
