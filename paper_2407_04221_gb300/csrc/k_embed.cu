@@ -678,8 +678,8 @@ int bits_of(int64_t V)
 }
 
 // Places a tile: as many as let the groups of all tiles run at once (three blocks of eight warps an SM), or in a few equal
-// turns; a multiple of eight, 128 at most.  (262,144 rows of 256 values: 46 us with tiles of 64, whose 512 blocks come for
-// 456 places, and 36 with tiles of 72.)
+// turns; a multiple of eight, 128 at most.  (262,144 rows of 256 values: 43 us with tiles of 64, whose 512 blocks come for
+// 456 places, and 33 with tiles of 72; 30,011 of 2,048 38 and 30.)
 int span_of(int64_t rows, int64_t D)
 {
     // groups of lanes for a tile, in 32nds of a warp, eight values a lane

@@ -11,7 +11,8 @@
 // to the workspace (the logits whole would be 2 GB at 8,192 x 65,536), from where
 // two products take it: dw of the piece, and what the piece adds to dx, summed in
 // 32 bits over the pieces.  G goes as two values of 16 bits, the rounded one and
-// what that leaves, so that only dx and dw are rounded: 10 N V D operations where
+// what that leaves, and sums of 512 terms are added in 32 bits, as those of 256 are
+// of the logits, so that only dx and dw are rounded: 10 N V D operations where
 // one value would take 6, and the error of rounding once in place of 1.41 times
 // it.  float16 has not the range for G: it goes times a power of two, from the
 // largest |dlogp|, and the results are brought back before they are rounded.
@@ -164,8 +165,9 @@ __global__ __launch_bounds__(kRowsThreads) void head_rows_kernel(int rows, int64
         *shared = {base, scale};
 }
 
-// Rows of which every block looks at all tokens.  16,384 x 256 x 4,096 forward and back 43.3 and 189 us, in two steps 47.5 and
-// 205; 1,024 12.9 and 33.1, and 14.7 and 37.1.
+// Rows of which every block looks at all tokens.  Forward and back, of 64 columns and 256 words: 16,384 rows 19 and 49 us, in
+// two steps 22 and 63; 32,768 31 and 72, and 33 and 101; 65,536 64 and 137, and 56 and 178; 131,072 179 and 310, and 98 and
+// 332; 262,144 587 and 830, and 186 and 640.  One number for both passes.
 constexpr int kOnceRows = 32768;
 constexpr int kOnceThreads = 256;
 constexpr int kOnceEach = 64;     // rows of a block
@@ -324,7 +326,7 @@ struct Tile {
 
 // Blocks of 64 terms that accumulators take before they are added to sums in registers, of logits.  The tensor cores
 // truncate at every addition to the accumulator, a bias that grows with their number: of 8,192 x 1,024 x 65,536 the peaks
-// are off by 1.1e-6 of themselves, as root mean square, with all terms at once (616 us), by 5.2e-7 with eight blocks
+// are off by 1.1e-6 of themselves, as root mean square, with all terms at once (the call 616 us), by 5.2e-7 with eight blocks
 // (632), 2.5e-7 with four (670; sums in 32 bits 3.2e-7) and 1.3e-7 with two (783).  Backward they are the same sums, to the
 // last bit: m and logz are of them, and in a row that is sure of its token what is left of one, 1 - p, is of the size of
 // such errors (2.5 % of that call's gradient: 3.60 ms with all terms at once, 3.69 with these).
@@ -355,9 +357,9 @@ __device__ __forceinline__ Tile tile_of(const Work &p, int i)
 }
 
 // Which tiles a pair takes: the longer product's go round the pairs; of the other's the pairs that came away with one less
-// take as many ahead as make up for it, and the rest go round.  How many rows have a token is known on the GPU alone: of
-// 2,999 x 520 x 50,021, a third of the rows without one, the gradient takes 514 us, and 589 with both products' tiles
-// going round.
+// take as many ahead as make up for it, and the rest go round.  How many rows have a token is known on the GPU alone.  The
+// gradient of 16,384 x 512 x 32,768 takes 1.97 ms, and 2.25 with both products' tiles going round; of 2,999 x 520 x 50,021, a
+// third of the rows without a token, 555 us and 571.
 struct Turns {
     int pair, pairs, longer, shorter, rest, ahead;  // tiles; pairs with one more of the longer; tiles taken ahead
     __device__ __forceinline__ Turns(int n_longer, int n_shorter, int long_blocks, int short_blocks)
@@ -399,9 +401,9 @@ __device__ __forceinline__ void join(float2 &a, float2 b)
 }
 
 // Logits: A is x (or packed), B w.  Products: of G (by its rows and by its columns) with w, and with x (or packed).
-// 8,192 x 1,024 x 65,536, bf16: all logits 640 us (1.72 PFLOP/s, tensor cores active 74 % of the cycles); of 9,728 words G
-// 121 us (62 %: a tile's stores, 128 KB a CTA, and what leads up to them take longer than its products), the products 390
-// (1.67 PFLOP/s, 84 %, at the clock that power leaves).
+// 8,192 x 1,024 x 65,536, bf16: all logits 640 us (1.72 PFLOP/s, tensor cores active 71 % of the cycles); of 9,728 words G
+// 133 us (55 %: a tile's stores, 128 KB a CTA, and what leads up to them take longer than its products), the products 411
+// (1.59 PFLOP/s, 76 %, at the clock that power leaves).
 template <class T, int kForm>
 __global__ __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kForm), 1) void head_kernel(
     const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap packed_map,
@@ -1078,8 +1080,8 @@ double deal(int64_t rows, int64_t words, int64_t D, int &dx_splits, int &dw_spli
     return least;
 }
 
-// Values of G at once: 470 MB as two.  Backward, with 134, 336, 470 and 671 MB: 8,192 x 256 x 32,768 719, 654 to 679, 614
-// and 608 us, 16,384 x 512 x 32,768 2.21, 1.99 to 2.07, 1.93 and 1.94 ms; 8,192 x 1,024 x 65,536 some 3.65 ms with any.
+// Values of G at once: 470 MB as two.  Backward, with 134, 336, 470 and 671 MB: 8,192 x 256 x 32,768 770, 724, 665 and
+// 654 us, 16,384 x 512 x 32,768 2.32, 2.01, 1.97 and 1.93 ms; 8,192 x 1,024 x 65,536 3.95, 3.86, 3.82 and 3.71.
 constexpr int64_t kPieceValues = int64_t(7) << 24;
 
 // Words at once: the number that ends soonest, of those that leave G in its room.  (With room for 336 MB, 2,999 x 520 x
