@@ -494,7 +494,9 @@ int av_gated_ffn(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act,
  * second what rounding the first leaves, so that only the results are rounded.
  * Of AV_F16 they go times a power of two that keeps the largest in range: a
  * result is infinite where it is itself beyond the type, and values down to
- * 2^-36 of the largest gradient of a projection count. */
+ * 2^-36 of the largest gradient of a projection count.  The tensor cores truncate
+ * their sums at every addition: sums of one sign are short, dw of 65,536 rows by
+ * 2.1e-4 of itself, dx of 4,096 channels by 6e-5. */
 int av_gated_ffn_grad(int64_t rows, int64_t D, int64_t H, int32_t dtype, int32_t act, const void *dh,
                       int64_t dh_stride, const void *x, int64_t x_stride, const void *w, void *dx,
                       int64_t dx_stride, void *dw, void *work, int64_t work_bytes,
